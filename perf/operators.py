@@ -1,0 +1,412 @@
+"""Two operators beside the sparse memory layer, as a program calls them, and their plain forms.
+
+``delta``: the dense gated delta rule, the recurrence that the sparse layer's table replaces.  Per stream (b, h)
+with a state S of d_k x d_v values and t = 0 .. T-1::
+
+    S <- alpha_t S;  e = beta_t (v_t - S^T k_t);  S <- S + k_t e^T;  y_t = S^T q_t
+
+``linear``: the projections around either layer, ``y = act(x W^T + bias) + residual``, from and to the layers'
+head-major layout [B, H, T, d], and its gradients.
+
+``run`` takes the framework's calls where ``own`` is true and elementary torch operations in fp32 otherwise.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+CHUNK = 64          # tokens per chunk of the plain form
+NONE, SILU, GELU = 0, 1, 2
+DEV = "cuda"
+
+
+# ------------------------------------------------------------------------------------------------ cases
+def _delta(name, do, B, Hk, H, T, d_k, d_v, bf16=True, ragged=False, start=False):
+    return dict(name=name, op="delta", do=do, B=B, Hk=Hk, H=H, T=T, d_k=d_k, d_v=d_v, bf16=bf16, ragged=ragged,
+                start=start)
+
+
+def _linear(name, do, B, T, K, N, act=NONE, bias=False, residual=False, heads_in=0, heads_out=0, bf16=True,
+            x_f32=False):
+    return dict(name=name, op="linear", do=do, B=B, T=T, K=K, N=N, act=act, bias=bias, residual=residual,
+                heads_in=heads_in, heads_out=heads_out, bf16=bf16, x_f32=x_f32)
+
+
+def listed():
+    return [
+        # One user waits for one token: 16 heads of one layer.  Latency only.
+        _delta("delta_decode_one", "forward", 1, 16, 16, 1, 128, 128, start=True),
+        # Serving: one token for each of 16 sequences (the benchmark's decode step, with the dense state).
+        _delta("delta_decode", "forward", 16, 16, 16, 1, 128, 128, start=True),
+        # Prompts of a padded batch in fp32, of lengths and sizes that nobody chose; two value heads share a key head.
+        _delta("delta_prompts_ragged_f32", "forward", 5, 4, 8, 777, 72, 100, bf16=False, ragged=True, start=True),
+        # The benchmark's forward shape: eight sequences of 4096 tokens, 16 heads of 128.
+        _delta("delta_forward", "forward", 8, 16, 16, 4096, 128, 128),
+        # One document of 65,536 tokens: few streams, many chunks one after the other.
+        _delta("delta_long", "forward", 1, 16, 16, 65536, 128, 128),
+        # The benchmark's training shape: forward with the states kept, then the backward.
+        _delta("delta_train", "train", 4, 16, 16, 4096, 128, 128),
+        # A small training step in fp32 on a padded batch, three value heads to a key head.
+        _delta("delta_train_shared_f32", "train", 2, 2, 6, 333, 64, 96, bf16=False, ragged=True, start=True),
+        # One token of 16 sequences through a projection with its activation.
+        _linear("linear_decode", "forward", 16, 1, 2048, 2048, act=SILU, bias=True, heads_out=16),
+        # Input projection of a training batch: written head-major, as the layers read it.
+        _linear("linear_project", "forward", 4, 4096, 2048, 2048, act=SILU, heads_out=16),
+        # Output projection: the epilogue's fp32 rows, head-major, mixed over the heads and added to the stream.
+        _linear("linear_mix_heads", "forward", 4, 4096, 2048, 2048, residual=True, heads_in=16, x_f32=True),
+        # The input projection's training step: forward that keeps the pre-activation, then all gradients.
+        _linear("linear_train", "train", 4, 4096, 2048, 2048, act=SILU, bias=True, heads_out=16),
+        # A training step in fp32 whose sizes divide nothing.
+        _linear("linear_train_odd_f32", "train", 3, 777, 500, 350, act=GELU, bias=True, bf16=False),
+    ]
+
+
+def _spread(rng, lo, hi):
+    """A whole number, uniform in the logarithm."""
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _draw_delta(rng):
+    do = rng.choice(["forward", "forward", "train"])
+    most = (8 if do == "forward" else 4) * 16 * 4096 * 128 * 128
+    while True:
+        T = rng.choice([1, _spread(rng, 1, 64), _spread(rng, 1, 4096), _spread(rng, 64, 16384 if do == "forward" else 4096)])
+        Hk, G = rng.randint(1, 16), rng.choice([1, 1, 2, 3, 4])
+        d = rng.choice([64, 128, 256])
+        d_k, d_v = (d, d) if rng.random() < 0.4 else (4 * _spread(rng, 4, 64), 4 * _spread(rng, 4, 64))
+        B = _spread(rng, 1, 64)
+        if B * Hk * G * T * d_k * d_v <= most and B * Hk * G * d_k * d_v <= 1 << 26:
+            return dict(op="delta", do=do, B=B, Hk=Hk, H=Hk * G, T=T, d_k=d_k, d_v=d_v, bf16=rng.random() < 0.7,
+                        ragged=rng.random() < 0.4, start=rng.random() < 0.5)
+
+
+def _draw_linear(rng):
+    do = rng.choice(["forward", "forward", "train"])
+    bf16 = rng.random() < 0.7
+    while True:
+        B, T = _spread(rng, 1, 32), rng.choice([1, _spread(rng, 1, 8192)])
+        heads_in = rng.choice([0, 0, rng.randint(1, 32)])
+        heads_out = rng.choice([0, 0, rng.randint(1, 32)])
+        K = heads_in * 8 * rng.randint(1, 32) if heads_in else 8 * _spread(rng, 4, 512)
+        N = heads_out * rng.randint(1, 256) if heads_out else _spread(rng, 1, 4096)
+        if B * T * K * N <= (16384 * 2048 * 2048 if bf16 else 2048 * 2048 * 2048) and B * T <= 32768:
+            return dict(op="linear", do=do, B=B, T=T, K=K, N=N, act=rng.choice([NONE, SILU, GELU]),
+                        bias=rng.random() < 0.5, residual=not heads_out and rng.random() < 0.5, heads_in=heads_in,
+                        heads_out=heads_out, bf16=bf16, x_f32=bf16 and do == "forward" and rng.random() < 0.3)
+
+
+def draw(rng):
+    return _draw_delta(rng) if rng.random() < 0.55 else _draw_linear(rng)
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+class _State:
+    pass
+
+
+def prepare(case, seed):
+    s = _State()
+    s.c = c = dict(case)
+    g = torch.Generator(device=DEV).manual_seed(int(seed) * 7919 + 17)
+    n = lambda *shape: torch.randn(shape, generator=g, device=DEV)          # noqa: E731
+    u = lambda *shape: torch.rand(shape, generator=g, device=DEV)           # noqa: E731
+    dt = torch.bfloat16 if c["bf16"] else torch.float32
+    if c["op"] == "delta":
+        B, Hk, H, T, d_k, d_v = (c[x] for x in ("B", "Hk", "H", "T", "d_k", "d_v"))
+        unit = lambda x: (x / x.norm(dim=-1, keepdim=True)).to(dt)          # noqa: E731
+        s.q, s.k = unit(n(B, Hk, T, d_k)), unit(torch.nn.functional.silu(n(B, Hk, T, d_k)))
+        s.v = n(B, H, T, d_v).to(dt)
+        # gates at the layer's initialisation: A in [0, 16], time steps in [0.001, 0.1]
+        step = 0.001 + 0.099 * u(1, H, 1)
+        b_dt = step + torch.log(-torch.expm1(-step))
+        s.alpha = torch.exp(-16 * u(1, H, 1) * torch.nn.functional.softplus(0.5 * n(B, H, T) + b_dt))
+        s.beta = torch.sigmoid(n(B, H, T))
+        s.state0 = 0.3 * n(B, H, d_k, d_v) if c["start"] else None
+        s.lens = None
+        if c["ragged"]:
+            s.lens = torch.randint(0, T + 1, (B,), generator=g, device=DEV, dtype=torch.int32)
+            s.lens[0] = T
+            if B > 2:
+                s.lens[B - 1] = 0
+        if c["do"] == "train":
+            s.dy, s.dstate = n(B, H, T, d_v), 0.3 * n(B, H, d_k, d_v)
+            if own:
+                from paper_2607_07386_amd import sdm
+                s.saved = sdm.gdn_saved_buffer(B, H, T, d_k, d_v, torch.device(DEV, torch.cuda.current_device()))
+        return s
+    B, T, K, N, hi, ho = (c[x] for x in ("B", "T", "K", "N", "heads_in", "heads_out"))
+    x = n(B, hi, T, K // hi) if hi else n(B, T, K)
+    s.x = x if c["x_f32"] else x.to(dt)
+    s.w = (n(N, K) / math.sqrt(K)).to(dt)
+    s.bias = 0.1 * n(N) if c["bias"] else None
+    s.residual = n(B, T, N).to(dt) if c["residual"] else None
+    if c["do"] == "train":
+        s.dy = (n(B, ho, T, N // ho) if ho else n(B, T, N)).to(dt)
+    return s
+
+
+# ------------------------------------------------------------------------------------------------ plain forms
+def _in_chunks(x):
+    """[B, H, T, ...] -> [B, H, n, CHUNK, ...], zeros past T."""
+    T = x.shape[2]
+    n = -(-T // CHUNK)
+    pad = x.new_zeros((*x.shape[:2], n * CHUNK - T, *x.shape[3:]))
+    return torch.cat([x, pad], 2).unflatten(2, (n, CHUNK))
+
+
+def _valid(s, T):
+    """[B, 1, T]: the tokens that belong to a sequence."""
+    at = torch.arange(T, device=DEV)[None, None]
+    return at < (T if s.lens is None else s.lens.long()[:, None, None])
+
+
+def _plain_delta(s):
+    """The chunk form: within a chunk the innovations e solve a unit lower-triangular system; chunks follow one
+    another through the state.  The decays between two tokens come from 64-bit sums of log alpha."""
+    c = s.c
+    T, G = c["T"], c["H"] // c["Hk"]
+    live = _valid(s, T)
+    q, k, v = (x.float() for x in (s.q, s.k, s.v))
+    q, k = (_in_chunks(x.repeat_interleave(G, 1) * live[..., None]) for x in (q, k))
+    v = _in_chunks(v * live[..., None])
+    b = _in_chunks(s.beta * live)
+    a = torch.where(live, s.alpha, torch.ones_like(s.alpha))
+    lam = _in_chunks(a.double().log()).cumsum(-1)
+    low = torch.ones((CHUNK, CHUNK), dtype=torch.bool, device=DEV).tril()
+    D = torch.where(low, (lam[..., :, None] - lam[..., None, :]).clamp(max=0), -torch.inf).exp().float()
+    gam, end = lam.exp().float()[..., None], (lam[..., -1:] - lam).exp().float()[..., None]
+    last = gam[..., -1:, :]
+    Nn = (k @ k.transpose(-1, -2) * D).tril(-1)
+    P = q @ k.transpose(-1, -2) * D
+    A = Nn * b[..., None, :]
+    inv = torch.eye(CHUNK, device=DEV).expand_as(A).contiguous()
+    for i in range(1, CHUNK):                       # row i of (I + A)^-1 from the rows above it
+        inv[..., i, :i] = -(A[..., i, :i, None] * inv[..., :i, :i]).sum(-2)
+    kg, qg, ke = k * gam, q * gam, k * end
+    n = k.shape[2]
+    S = s.state0.clone() if s.state0 is not None else v.new_zeros((*v.shape[:2], c["d_k"], c["d_v"]))
+    starts, xs, ys = [], [], []
+    for j in range(n):                              # the recurrence itself: a chunk needs the one before it
+        X = inv[:, :, j] @ (v[:, :, j] - kg[:, :, j] @ S)
+        E = b[:, :, j, :, None] * X
+        ys.append(qg[:, :, j] @ S + P[:, :, j] @ E)
+        if c["do"] == "train":
+            starts.append(S)
+            xs.append(X)
+        S = last[:, :, j] * S + ke[:, :, j].transpose(-1, -2) @ E
+    y = (torch.stack(ys, 2).flatten(2, 3)[:, :, :T] if ys else v[:, :, :0, 0]) * live[..., None]
+    out = dict(y=y, state=S)
+    if c["do"] != "train":
+        return out
+    dy = _in_chunks(s.dy * live[..., None])
+    dS = s.dstate
+    ends, drs = [None] * n, [None] * n
+    for j in reversed(range(n)):
+        ends[j] = dS
+        dE = P[:, :, j].transpose(-1, -2) @ dy[:, :, j] + ke[:, :, j] @ dS
+        dR = inv[:, :, j].transpose(-1, -2) @ (b[:, :, j, :, None] * dE)
+        drs[j] = dR
+        dS = last[:, :, j] * dS + qg[:, :, j].transpose(-1, -2) @ dy[:, :, j] - kg[:, :, j].transpose(-1, -2) @ dR
+    S0, S1, X, dR = torch.stack(starts, 2), torch.stack(ends, 2), torch.stack(xs, 2), torch.stack(drs, 2)
+    t = lambda m: m.transpose(-1, -2)               # noqa: E731
+    Z2, Z = (dy @ t(X)).tril(), (dR @ t(X)).tril(-1)
+    M1, M2, M3 = X @ t(S1), dy @ t(S0), dR @ t(S0)
+    bj = b[..., None, :]
+    Pg, Ng = Z2 * bj * D, Z * bj * D
+    dq = gam * M2 + Pg @ k
+    dk = t(Pg) @ q + b[..., None] * end * M1 - gam * M3 - (Ng + t(Ng)) @ k
+    to_end = end[..., 0] * (k * M1).sum(-1)
+    db = (P * Z2).sum(-2) + to_end - (Nn * Z).sum(-2)
+    # log alpha_t scales every pair (i, j) with j < t <= i, the start's part of every i >= t, the way to the end of
+    # every j < t, and the state's own way through the chunk
+    pairs = (P * Z2 - Nn * Z) * bj
+    before = pairs.cumsum(-1) - pairs               # [i, t]: pairs of i with j < t
+    # at [i, i]: j < i; at [i, t < i]: j < t
+    cross = before.tril().sum(-2)
+    from_start = gam[..., 0] * ((q * M2).sum(-1) - (k * M3).sum(-1))
+    through = (last[..., 0, 0] * (S0 * S1).sum((-1, -2)))[..., None]
+    ends_of = b * to_end
+    dlog = cross + from_start.flip(-1).cumsum(-1).flip(-1) + (ends_of.cumsum(-1) - ends_of) + through
+    flat = lambda x: x.flatten(2, 3)[:, :, :T]      # noqa: E731
+    shared = lambda x: flat(x).unflatten(1, (c["Hk"], G)).sum(2) * live[..., None]      # noqa: E731
+    out.update(dq=shared(dq), dk=shared(dk), dv=flat(dR) * live[..., None], dalpha=flat(dlog) / a * live,
+               dbeta=flat(db) * live, dstate0=dS)
+    return out
+
+
+def _act(z, act):
+    if act == SILU:
+        return z * torch.sigmoid(z)
+    return 0.5 * z * (1 + torch.erf(z / math.sqrt(2))) if act == GELU else z
+
+
+def _act_slope(z, act):
+    if act == SILU:
+        p = torch.sigmoid(z)
+        return p * (1 + z * (1 - p))
+    if act == GELU:
+        return 0.5 * (1 + torch.erf(z / math.sqrt(2))) + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+    return torch.ones_like(z)
+
+
+def _rows(x, heads):
+    """[B, T, d] or [B, H, T, d] -> [B T, H d]."""
+    return (x.transpose(1, 2) if heads else x).reshape(x.shape[0] * x.shape[2 if heads else 1], -1)
+
+
+def _unrows(x, B, T, heads):
+    return x.view(B, T, heads, -1).transpose(1, 2).contiguous() if heads else x.view(B, T, -1)
+
+
+def _linear_forms(s, wide):
+    """The projection (and, for training, its gradients) in the type `wide`, rounded once at the end."""
+    c = s.c
+    B, T, dt = c["B"], c["T"], s.w.dtype
+    x, w = _rows(s.x.to(wide), c["heads_in"]), s.w.to(wide)
+    z = x @ w.T
+    if s.bias is not None:
+        z = z + s.bias.to(wide)
+    y = _act(z, c["act"])
+    if s.residual is not None:
+        y = y + s.residual.to(wide).flatten(0, 1)
+    keep = (lambda m: m) if wide is torch.float64 else (lambda m: m.to(dt))             # noqa: E731
+    out = dict(y=_unrows(keep(y), B, T, c["heads_out"]))
+    if c["do"] == "train":
+        out["z"] = _unrows(keep(z), B, T, c["heads_out"])
+        dz = _rows(s.dy.to(wide), c["heads_out"]) * _act_slope(z, c["act"])
+        out["dx"] = _unrows(keep(dz @ w), B, T, c["heads_in"])
+        out["dw"] = keep(dz.T @ x)
+        if s.bias is not None:
+            out["dbias"] = dz.sum(0)
+    return out
+
+
+def run(s):
+    c = s.c
+    if not own:
+        return _plain_delta(s) if c["op"] == "delta" else _linear_forms(s, torch.float32)
+    from paper_2607_07386_amd import sdm
+    if c["op"] == "delta":
+        if c["do"] == "forward":
+            y, state = sdm.gdn_fwd(s.q, s.k, s.v, s.alpha, s.beta, s.state0, lens=s.lens)
+            return dict(y=y, state=state)
+        y, state = sdm.gdn_fwd(s.q, s.k, s.v, s.alpha, s.beta, s.state0, lens=s.lens, saved=s.saved)
+        g = sdm.gdn_bwd(s.q, s.k, s.v, s.alpha, s.beta, s.saved, s.dy, dstate_T=s.dstate, lens=s.lens)
+        return dict(y=y, state=state, **{x: g[x] for x in ("dq", "dk", "dv", "dalpha", "dbeta", "dstate0")})
+    if c["do"] == "forward":
+        return dict(y=sdm.linear(s.x, s.w, s.bias, act=c["act"], residual=s.residual, heads=c["heads_out"]))
+    y, z = sdm.linear(s.x, s.w, s.bias, act=c["act"], residual=s.residual, heads=c["heads_out"], want_z=True)
+    g = sdm.linear_bwd(s.x, s.w, s.dy, z=z, act=c["act"], want_dbias=s.bias is not None)
+    return dict(y=y, z=z, **{x: g[x] for x in ("dx", "dw", "dbias") if g[x] is not None})
+
+
+# ------------------------------------------------------------------------------------------------ work
+def work(c):
+    """Inputs once, outputs once; for the recurrence three products of d_k x d_v per token (read-back, write,
+    read) and seven in the backward."""
+    e = 2 if c["bf16"] else 4
+    if c["op"] == "delta":
+        B, Hk, H, T, d_k, d_v = (c[x] for x in ("B", "Hk", "H", "T", "d_k", "d_v"))
+        tok, st = B * H * T, B * H * d_k * d_v * 4
+        ins = 2 * B * Hk * T * d_k * e + tok * (d_v * e + 8)
+        by = ins + tok * d_v * 4 + st * (2 if c["start"] else 1)
+        fl = 6.0 * tok * d_k * d_v
+        if c["do"] == "train":
+            by += ins + tok * d_v * 4 + st + 2 * B * Hk * T * d_k * 4 + tok * (d_v + 2) * 4 + st
+            fl += 14.0 * tok * d_k * d_v
+        return {"bytes": by, "flops": fl}
+    M, K, N = c["B"] * c["T"], c["K"], c["N"]
+    by = M * K * (4 if c["x_f32"] else e) + N * K * e + M * N * e * (2 if c["residual"] else 1) + (4 * N if c["bias"] else 0)
+    fl = 2.0 * M * K * N
+    if c["do"] == "train":
+        by += M * N * e * 3 + M * K * e * 2 + N * K * e * 2 + (4 * N if c["bias"] else 0)
+        fl *= 3
+    return {"bytes": by, "flops": fl}
+
+
+# ------------------------------------------------------------------------------------------------ 64 bits
+def _exact_delta(s):
+    """The definition, token by token; the backward recomputes a block's states from its start."""
+    c = s.c
+    T, G, BLK = c["T"], c["H"] // c["Hk"], 64
+    live = _valid(s, T)
+    m = live[..., None]
+    q, k = (x.double().repeat_interleave(G, 1) * m for x in (s.q, s.k))
+    v, be = s.v.double() * m, s.beta.double() * live
+    al = torch.where(live, s.alpha, torch.ones_like(s.alpha)).double()
+    S = s.state0.double() if s.state0 is not None else v.new_zeros((*v.shape[:2], c["d_k"], c["d_v"]))
+
+    def step(S, t):
+        D = al[:, :, t, None, None] * S
+        kt = k[:, :, t, :, None]
+        w = v[:, :, t] - (kt * D).sum(-2)
+        return D, w, D + kt * (be[:, :, t, None] * w)[:, :, None]
+
+    y = torch.empty_like(v)
+    marks = []
+    for t in range(T):
+        if c["do"] == "train" and t % BLK == 0:
+            marks.append(S)
+        S = step(S, t)[2]
+        y[:, :, t] = (q[:, :, t, :, None] * S).sum(-2)
+    out = dict(y=y * m, state=S)
+    if c["do"] != "train":
+        return out
+    dy, Gs = s.dy.double() * m, s.dstate.double()
+    dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    da, db = torch.zeros_like(al), torch.zeros_like(be)
+    for j in reversed(range(len(marks))):
+        t0, t1 = j * BLK, min(T, (j + 1) * BLK)
+        chain = [(marks[j],)]
+        for t in range(t0, t1):
+            D, w, S1 = step(chain[-1][0], t)
+            chain.append((S1, D, w, chain[-1][0]))
+        for t in reversed(range(t0, t1)):
+            S1, D, w, S0 = chain[t - t0 + 1]
+            dyt, kt, bt = dy[:, :, t], k[:, :, t], be[:, :, t, None]
+            dq[:, :, t] = (S1 * dyt[:, :, None]).sum(-1)
+            Gs = Gs + q[:, :, t, :, None] * dyt[:, :, None]
+            ge = (Gs * kt[..., None]).sum(-2)
+            db[:, :, t] = (ge * w).sum(-1)
+            dv[:, :, t] = bt * ge
+            dk[:, :, t] = (Gs * (bt * w)[:, :, None]).sum(-1) - (D * (bt * ge)[:, :, None]).sum(-1)
+            dD = Gs - kt[..., None] * (bt * ge)[:, :, None]
+            da[:, :, t] = (dD * S0).sum((-1, -2))
+            Gs = al[:, :, t, None, None] * dD
+    shared = lambda x: (x * m).unflatten(1, (c["Hk"], G)).sum(2)            # noqa: E731
+    out.update(dq=shared(dq), dk=shared(dk), dv=dv * m, dalpha=da * live, dbeta=db * live, dstate0=Gs)
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "delta":
+        return _exact_delta(s)
+    c = case
+    if c["do"] == "train":      # through the definition's own derivative
+        wide = _State()
+        wide.__dict__.update(s.__dict__)
+        wide.c = dict(c, do="forward")
+        wide.x, wide.w = s.x.double().requires_grad_(), s.w.double().requires_grad_()
+        lead = [] if s.bias is None else [s.bias.double().requires_grad_()]
+        x = wide.x.transpose(1, 2).flatten(-2) if c["heads_in"] else wide.x
+        z = torch.nn.functional.linear(x, wide.w, *lead)
+        f = {NONE: lambda a: a, SILU: torch.nn.functional.silu, GELU: torch.nn.functional.gelu}[c["act"]](z)
+        to = (lambda a: a.unflatten(-1, (c["heads_out"], -1)).transpose(1, 2)) if c["heads_out"] else (lambda a: a)
+        got = torch.autograd.grad(to(f), [wide.x, wide.w, *lead], s.dy.double())
+        y = to(f) if s.residual is None else f + s.residual.double()
+        out = dict(y=y.detach(), z=to(z).detach(), dx=got[0], dw=got[1])
+        if lead:
+            out["dbias"] = got[2]
+        return out
+    x = s.x.double()
+    if c["heads_in"]:
+        x = x.transpose(1, 2).flatten(-2)
+    z = torch.nn.functional.linear(x, s.w.double(), None if s.bias is None else s.bias.double())
+    y = {NONE: lambda a: a, SILU: torch.nn.functional.silu, GELU: torch.nn.functional.gelu}[c["act"]](z)
+    if c["heads_out"]:
+        y = y.unflatten(-1, (c["heads_out"], -1)).transpose(1, 2)
+    return dict(y=y if s.residual is None else y + s.residual.double())
