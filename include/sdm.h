@@ -400,6 +400,60 @@ int sdm_layer_bwd(const void* cb_q, const void* cb_k, int cb_dtype, int d_k,
                   float* dg, float* dgamma, float* dmem0, void* workspace, size_t ws_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * sdm_gdn_fwd — the dense gated delta rule (Sec. 2, Eq. gdn-update), the
+ * recurrence whose key-value state the sparse table replaces (Sec. 3.1
+ * "Connection to GDN").  Per stream (b, h) with a state S of d_k x d_v values,
+ * t = 0 .. len_b - 1:
+ *   S <- alpha_t S;  e = beta_t (v_t - S^T k_t);  S <- S + k_t e^T;  y_t = S^T q_t
+ *   q, k          [B, Hk, T, d_k] in in_dtype; head h reads key head h / (H / Hk)
+ *                 (H a multiple of Hk).  Taken as they are: the update contracts
+ *                 where beta |k|^2 <= 2, so callers normalise their keys.
+ *   v             [B, H, T, d_v] in in_dtype.
+ *   alpha, beta   [B, H, T] fp32, as sdm_gates writes them; alpha >= 0.
+ *   lens          [B] int32 or NULL (T for every sequence): tokens of each sequence
+ *                 of a padded batch, clamped to [0, T] on the device.  Rows of y
+ *                 past a sequence's end are left as they were, whatever the
+ *                 inputs hold there.
+ *   state0        [B, H, d_k, d_v] fp32 or NULL (zeros);  stateT  out, same shape,
+ *                 the state after the last token; may be the same buffer.
+ *   y             out [B, H, T, d_v] fp32.
+ *   saved         NULL, or for training a buffer of sdm_gdn_saved_bytes() bytes
+ *                 that sdm_gdn_bwd reads: the states at the starts of the 64-token
+ *                 chunks and the rows v_t - S^T k_t.
+ *   workspace     at least sdm_gdn_fwd_workspace_bytes() bytes, 256-B aligned;
+ *                 NULL where that is 0.
+ * Few tokens (the decode step T = 1 among them) run one launch that keeps the
+ * state in registers; longer sequences the chunk form of App. A.1, whose decays
+ * are logarithms: a gate below 1e-20 counts as 1e-20 there.  All products are
+ * fp32 (bf16 inputs are exact); the two forms agree to rounding.  Results do not
+ * depend on scheduling and are the same from run to run.
+ * Limits: d_k, d_v % 4 == 0; d_k <= 256; d_v <= 4096; B H <= 65535.
+ * ---------------------------------------------------------------------- */
+int sdm_gdn_fwd(const void* q, const void* k, const void* v, int in_dtype, const float* alpha, const float* beta,
+                const int32_t* lens, const float* state0, float* stateT, int B, int Hk, int H, int T, int d_k,
+                int d_v, float* y, void* saved, size_t saved_bytes, void* workspace, size_t ws_bytes, void* stream);
+size_t sdm_gdn_fwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v, int in_dtype, int training);
+size_t sdm_gdn_saved_bytes(int B, int H, int T, int d_k, int d_v);
+
+/* ------------------------------------------------------------------------
+ * sdm_gdn_bwd — reverse mode of sdm_gdn_fwd.  Inputs as given to it, `saved` as
+ * it left it (with saved != NULL), and
+ *   dy            [B, H, T, d_v] fp32: gradient of y (not read past a sequence's end);
+ *   dstateT       [B, H, d_k, d_v] fp32 gradient of stateT, or NULL (zeros);
+ *   dq, dk        out [B, Hk, T, d_k] fp32, summed over the heads that share a key
+ *                 head in order;  dv  out [B, H, T, d_v];  dalpha, dbeta  out
+ *                 [B, H, T];  dstate0  optional out [B, H, d_k, d_v], may be dstateT.
+ * Rows past a sequence's end are left as they were.  Where a gate below 1e-20
+ * counts as 1e-20 in the forward, dalpha is the gradient at 1e-20.
+ *   workspace     at least sdm_gdn_bwd_workspace_bytes() bytes, 256-B aligned.
+ * ---------------------------------------------------------------------- */
+int sdm_gdn_bwd(const void* q, const void* k, const void* v, int in_dtype, const float* alpha, const float* beta,
+                const int32_t* lens, const void* saved, size_t saved_bytes, const float* dy, const float* dstateT,
+                int B, int Hk, int H, int T, int d_k, int d_v, float* dq, float* dk, float* dv, float* dalpha,
+                float* dbeta, float* dstate0, void* workspace, size_t ws_bytes, void* stream);
+size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v, int in_dtype);
+
+/* ------------------------------------------------------------------------
  * sdm_mem_init — initial memory per call.  The learned initial state M_0 of
  * Sec. 3.1 ("Learned Initial State") is one [H, N, d_v] parameter shared by
  * all sequences; every sequence starts from its own copy:
@@ -481,7 +535,8 @@ enum sdm_kernel {
     SDM_K_ADDRESS = 0, SDM_K_FWD_PREP = 1, SDM_K_FWD_SCAN = 2, SDM_K_BWD_PREP = 3,
     SDM_K_BWD_SCAN = 4, SDM_K_BWD_REDUCE = 5, SDM_K_ADDRESS_BWD = 6, SDM_K_MEM_INIT = 7,
     SDM_K_DECODE = 8, SDM_K_CHUNK_COEF = 9, SDM_K_CHUNK_SCAN = 10, SDM_K_NORM_GATE = 11, SDM_K_GATES = 12,
-    SDM_K_COUNT = 13
+    SDM_K_GDN_PREP = 13, SDM_K_GDN_SCAN = 14, SDM_K_GDN_STEP = 15, SDM_K_GDN_BWD = 16,
+    SDM_K_COUNT = 17
 };
 int sdm_profile_enable(int on);
 /* Which kernel kinds the events bracket while profiling is enabled: bit k for

@@ -1,0 +1,518 @@
+// The dense gated delta rule, forward (gfx950).  Per stream (b, h) with a state S
+// of d_k x d_v values and t = 0 .. T-1 (Sec. 2, Eq. gdn-update; the recurrence
+// whose key-value state the sparse table replaces, Sec. 3.1 "Connection to GDN"):
+//   S <- alpha_t S;  e_t = beta_t (v_t - S^T k_t);  S <- S + k_t e_t^T;  y_t = S^T q_t
+//
+// Recurrent form (gdn_step_kernel): few tokens.  One pass over the state, which
+// stays in registers; with u = S^T k, w = S^T q of the state before the token,
+// y = alpha w + <k, q> e, so a token needs one reduction over the rows.
+//
+// Chunk form: tokens by 64.  With lambda_i the sum of log alpha up to token i of
+// the chunk, gamma_i = exp(lambda_i), D_ij = exp(lambda_i - lambda_j) for j <= i:
+//   N = stril(K K^T . D),  P = tril(Q K^T . D),  T' = (I + N diag(beta))^-1
+//   X = T' (V - diag(gamma) K S0)          (X_t = v_t - its read-back)
+//   E = diag(beta) X
+//   Y = diag(gamma) Q S0 + P E
+//   S1 = gamma_63 S0 + K^T diag(exp(lambda_63 - lambda)) E
+// gdn_prep_kernel makes T' and P of all chunks in parallel; gdn_scan_kernel walks
+// the chunks of a stream, one wave per 16 columns of the state.
+#include <algorithm>
+
+#include "gdn.h"
+#include "sdm_internal.h"
+
+namespace {
+
+// ---------------------------------------------------------------- recurrent
+// A workgroup holds 32 columns of one stream: 8 quads of columns x 32 row
+// groups, rows rg + 32 i in registers.
+template <typename VT, int NR>
+__global__ __launch_bounds__(256) void gdn_step_kernel(GdnArgs a) {
+    __shared__ float red[2][4][8][9];
+    const int bh = blockIdx.y, b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    const int cq = lane & 7, rg = (lane >> 3) + 8 * wave;
+    const int col = blockIdx.x * 32 + cq * 4;
+    const bool cv = col < a.dv;
+    const int len = gdn_len(a, b);
+    const size_t sbase = (size_t)bh * a.dk * a.dv;
+    v4f S[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+        const int r = rg + 32 * i;
+        S[i] = a.state0 && cv && r < a.dk ? ld4(a.state0 + sbase + (size_t)r * a.dv + col) : v4zero();
+    }
+    const size_t tq = (size_t)(b * a.Hk + hk) * a.T, tv = (size_t)bh * a.T;
+    const VT* kp = static_cast<const VT*>(a.k) + tq * a.dk;
+    const VT* qp = static_cast<const VT*>(a.q) + tq * a.dk;
+    const VT* vp = static_cast<const VT*>(a.v) + tv * a.dv + col;
+    for (int t = 0; t < len; ++t) {
+        float kr[NR], qr[NR];
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = rg + 32 * i;
+            const bool ok = r < a.dk;
+            kr[i] = ok ? to_f32(kp[(size_t)t * a.dk + r]) : 0.f;
+            qr[i] = ok ? to_f32(qp[(size_t)t * a.dk + r]) : 0.f;
+        }
+        const v4f vt = cv ? ld4v(vp + (size_t)t * a.dv) : v4zero();
+        const float al = a.alpha[tv + t], be = a.beta[tv + t];
+        v4f u = v4zero(), w = v4zero();
+        float kq = 0.f;
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            u = v4fma(kr[i], S[i], u);
+            w = v4fma(qr[i], S[i], w);
+            kq = fmaf(kr[i], qr[i], kq);
+        }
+#pragma unroll
+        for (int m = 8; m <= 32; m <<= 1) {
+            u += v4shfl_xor(u, m);
+            w += v4shfl_xor(w, m);
+            kq += xor_lane_f(kq, m);
+        }
+        float(&rd)[4][8][9] = red[t & 1];   // two of them: one barrier a token
+        if (lane < 8) {
+            float* p = rd[wave][cq];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[i] = u[i];
+                p[4 + i] = w[i];
+            }
+            p[8] = kq;
+        }
+        __syncthreads();
+        u = v4zero();
+        w = v4zero();
+        kq = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float* p = rd[j][cq];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                u[i] += p[i];
+                w[i] += p[4 + i];
+            }
+            kq += p[8];
+        }
+        v4f e, y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[i] = be * (vt[i] - al * u[i]);
+            y[i] = fmaf(kq, e[i], al * w[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            v4f n;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) n[j] = fmaf(kr[i], e[j], al * S[i][j]);
+            S[i] = n;
+        }
+        if (cv && rg == 0) st4(a.y + (tv + t) * a.dv + col, y);
+    }
+    if (a.stateT && cv) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = rg + 32 * i;
+            if (r < a.dk) st4(a.stateT + sbase + (size_t)r * a.dv + col, S[i]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- prep
+constexpr int LD = 68;   // row stride of the 64x64 fp32 matrices in LDS
+
+// one 16x16x16 product of fp32 matrices in LDS: acc += A[ar..][ac..] B[br..][bc..]
+__device__ __forceinline__ sdm_f32x4 lds_mm16(const float* A, int ar, int ac, const float* Bm, int br, int bc,
+                                              int ldb, sdm_f32x4 acc) {
+    const int r = lane_id() & 15, g = lane_id() >> 4;
+#pragma unroll
+    for (int k = 0; k < 16; k += 4)
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(A[(ar + r) * LD + ac + k + g], Bm[(br + k + g) * ldb + bc + r],
+                                                   acc, 0, 0, 0);
+    return acc;
+}
+
+// One workgroup per (stream, chunk).  T' by blocks: the four 16x16 diagonal
+// blocks by substitution (a lane per column), then the blocks below them from
+// products, T'_21 = -T'_22 A_21 T'_11, first within each half, then between.
+template <typename VT, int KTN, bool BWD>
+__global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
+    constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN;
+    __shared__ float M[64 * LD], Ti[64 * LD], P[64 * LD], W[32 * 36];
+    __shared__ float vlh[64], vll[64], vb[64];
+    const int c = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh % a.H;
+    const int G = a.H / a.Hk, hk = h / G;
+    const int len = gdn_len(a, b), t0 = c * GDN_C;
+    if (t0 >= len) return;
+    const int lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+    const size_t ch = (size_t)bh * a.nC + c;
+
+    if (w == 0) {
+        const int t = t0 + lane;
+        const bool ok = t < len;
+        float al = ok ? a.alpha[(size_t)bh * a.T + t] : 1.f;
+        al = al < GDN_ALPHA_MIN ? GDN_ALPHA_MIN : al;
+        const float be = ok ? a.beta[(size_t)bh * a.T + t] : 0.f;
+        double lam = log((double)al);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const double o = __shfl_up(lam, m, 64);
+            if (lane >= m) lam += o;
+        }
+        const double end = __shfl(lam, 63, 64);
+        const float hi = (float)lam, lo = (float)(lam - (double)hi);
+        vlh[lane] = hi;
+        vll[lane] = lo;
+        vb[lane] = be;
+        float* vec = a.vec + ch * GDN_VEC * 64;
+        vec[GDN_V_LHI * 64 + lane] = hi;
+        vec[GDN_V_LLO * 64 + lane] = lo;
+        vec[GDN_V_GAM * 64 + lane] = (float)exp(lam);
+        vec[GDN_V_END * 64 + lane] = (float)exp(end - lam);
+        vec[GDN_V_BETA * 64 + lane] = be;
+        vec[GDN_V_ALPHA * 64 + lane] = al;
+    }
+    // Gram matrices: this wave's 16 rows against the rows of blocks 0 .. w
+    const size_t tq = (size_t)(b * a.Hk + hk) * a.T + t0;
+    const VT* kp = static_cast<const VT*>(a.k) + tq * a.dk;
+    const VT* qp = static_cast<const VT*>(a.q) + tq * a.dk;
+    sdm_f32x4 kk[4], qk[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) kk[j] = qk[j] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = 16 * w + r16;
+    for (int kb = 0; kb < KTN; ++kb) {
+        const bool ok = t0 + row < len;
+        const GdnFrag<NT> fk = gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, ok);
+        const GdnFrag<NT> fq = gdn_row_frag<NT>(qp + (size_t)row * a.dk, kb, a.dk, ok);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j > w) break;
+            const int rj = 16 * j + r16;
+            const GdnFrag<NT> fb = gdn_row_frag<NT>(kp + (size_t)rj * a.dk, kb, a.dk, t0 + rj < len);
+            kk[j] = gdn_mm(fk, fb, kk[j]);
+            qk[j] = gdn_mm(fq, fb, qk[j]);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int cj = 16 * j + r16;
+        const float bj = vb[cj], hj = vlh[cj], lj = vll[cj];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * w + 4 * g + r;
+            float n = 0.f, p = 0.f;
+            if (cj <= i) {
+                const float d = gdn_decay(vlh[i], vll[i], hj, lj);
+                n = cj < i ? kk[j][r] * d : 0.f;
+                p = qk[j][r] * d;
+            }
+            M[i * LD + cj] = n * bj;
+            P[i * LD + cj] = p;
+            Ti[i * LD + cj] = 0.f;
+            if constexpr (BWD) {
+                a.pm[(ch * 64 + i) * 64 + cj] = p;
+                a.nm[(ch * 64 + i) * 64 + cj] = n;
+            }
+        }
+    }
+    __syncthreads();
+    if (lane < 16) {   // diagonal block w, column `lane`
+        const int o = 16 * w;
+        float x[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float s = i == lane ? 1.f : 0.f;
+#pragma unroll
+            for (int l = 0; l < i; ++l) s = fmaf(-M[(o + i) * LD + o + l], x[l], s);
+            x[i] = s;
+            Ti[(o + i) * LD + o + lane] = s;
+        }
+    }
+    __syncthreads();
+    const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    if (w < 2) {       // W <- A_21 T'_11 within half w
+        const sdm_f32x4 t = lds_mm16(M, 32 * w + 16, 32 * w, Ti, 32 * w, 32 * w, LD, zero);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) W[(16 * w + 4 * g + r) * 36 + r16] = t[r];
+    }
+    __syncthreads();
+    if (w < 2) {
+        const sdm_f32x4 t = lds_mm16(Ti, 32 * w + 16, 32 * w + 16, W, 16 * w, 0, 36, zero);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Ti[(32 * w + 16 + 4 * g + r) * LD + 32 * w + r16] = -t[r];
+    }
+    __syncthreads();
+    {                  // between the halves: 32x32, a 16x16 tile per wave
+        const int ti = w >> 1, tj = w & 1;
+        sdm_f32x4 t = lds_mm16(M, 32 + 16 * ti, 0, Ti, 0, 16 * tj, LD, zero);
+        t = lds_mm16(M, 32 + 16 * ti, 16, Ti, 16, 16 * tj, LD, t);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) W[(16 * ti + 4 * g + r) * 36 + 16 * tj + r16] = t[r];
+        __syncthreads();
+        t = lds_mm16(Ti, 32 + 16 * ti, 32, W, 0, 16 * tj, 36, zero);
+        t = lds_mm16(Ti, 32 + 16 * ti, 48, W, 16, 16 * tj, 36, t);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Ti[(32 + 16 * ti + 4 * g + r) * LD + 16 * tj + r16] = -t[r];
+    }
+    __syncthreads();
+    // fragments of T' and P (backward: of their transposes): 6 blocks each
+    for (int f = w; f < 2 * GDN_BLKS; f += 4) {
+        const int blk = f % GDN_BLKS;
+        const float* src = f < GDN_BLKS ? Ti : P;
+        int mt, kb;
+        if constexpr (BWD) {
+            mt = blk < 4 ? blk >> 1 : blk - 2;
+            kb = blk < 4 ? blk & 1 : 1;
+        } else {
+            mt = blk < 2 ? blk : 2 + ((blk - 2) >> 1);
+            kb = blk < 2 ? 0 : (blk - 2) & 1;
+        }
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int rr = 16 * mt + r16, cc = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+            x[i] = BWD ? src[cc * LD + rr] : src[rr * LD + cc];
+        }
+        gdn_store_frag<3>(f < GDN_BLKS ? a.tf : a.pf, ch * GDN_BLKS + blk, gdn_split(x));
+    }
+    // K^T (and Q^T) of the key head: rows of d_k, depth = tokens
+    if (h % G == 0) {
+        const size_t ck = (size_t)(b * a.Hk + hk) * a.nC + c;
+        for (int f = w; f < (BWD ? 2 : 1) * DT * 2; f += 4) {
+            const int id = f % (DT * 2), dt = id >> 1, kb = id & 1;
+            const VT* src = f < DT * 2 ? kp : qp;
+            const int d = 16 * dt + r16;
+            GdnFrag<NT> fr;
+            if constexpr (NT == 1) {
+                union {
+                    uint16_t u[8];
+                    sdm_bf16x8 v;
+                } x;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+                    x.u[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d].bits : (uint16_t)0;
+                }
+                fr.t[0] = x.v;
+            } else {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int t = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+                    x[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d] : 0.f;
+                }
+                fr = gdn_split(x);
+            }
+            gdn_store_frag<NT>(f < DT * 2 ? a.kt : a.qt, ck * DT * 2 + id, fr);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- scan
+// One wave per 16 columns of a stream's state, four to a workgroup; the waves
+// share nothing (each reads the chunk's fragments itself) and never wait for
+// one another.  The state stays in the C layout of its own update.
+template <typename VT, int KTN, bool SAVE>
+__global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
+    constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN;
+    const int groups = (a.dv + 63) / 64;
+    int grp, bh;
+    scan_wg_coords<true>(groups, grp, bh);
+    const int col0 = (grp * 4 + (threadIdx.x >> 6)) * 16;
+    if (col0 >= a.dv) return;
+    const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
+    const int lane = lane_id(), r16 = lane & 15, g = lane >> 4;
+    const int col = col0 + r16;
+    const bool cv = col < a.dv;
+    const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
+    const size_t sbase = (size_t)bh * a.dk * a.dv + col;
+    const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    sdm_f32x4 S[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * d + 4 * g + r;
+            S[d][r] = a.state0 && cv && row < a.dk ? a.state0[sbase + (size_t)row * a.dv] : 0.f;
+        }
+    const size_t tq0 = (size_t)(b * a.Hk + hk) * a.T, tv0 = (size_t)bh * a.T;
+    for (int c = 0; c < nc; ++c) {
+        const int t0 = c * GDN_C;
+        const size_t ch = (size_t)bh * a.nC + c, ck = (size_t)(b * a.Hk + hk) * a.nC + c;
+        const VT* kp = static_cast<const VT*>(a.k) + (tq0 + t0) * a.dk;
+        const VT* qp = static_cast<const VT*>(a.q) + (tq0 + t0) * a.dk;
+        const VT* vp = static_cast<const VT*>(a.v) + (tv0 + t0) * a.dv + col;
+        const float* vec = a.vec + ch * GDN_VEC * 64;
+        if constexpr (SAVE) {
+            float* o = a.saved_S + ch * a.dk * a.dv + col;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = 16 * d + 4 * g + r;
+                    if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
+                }
+        }
+        sdm_f32x4 R[4], Y[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) R[m] = Y[m] = zero;
+#pragma unroll
+        for (int kb = 0; kb < KTN; ++kb) {
+            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const int row = 16 * m + r16;
+                const bool ok = t0 + row < len;
+                R[m] = gdn_mm(gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, ok), s, R[m]);
+                Y[m] = gdn_mm(gdn_row_frag<NT>(qp + (size_t)row * a.dk, kb, a.dk, ok), s, Y[m]);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f gam = ld4(vec + GDN_V_GAM * 64 + 16 * m + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * m + 4 * g + r;
+                const float v = cv && t0 + t < len ? to_f32(vp[(size_t)t * a.dv]) : 0.f;
+                R[m][r] = fmaf(-gam[r], R[m][r], v);
+                Y[m][r] *= gam[r];
+            }
+        }
+        sdm_f32x4 X[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) X[m] = zero;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(R[2 * kb], R[2 * kb + 1]);
+#pragma unroll
+            for (int m = 2 * kb; m < 4; ++m)
+                X[m] = gdn_mm(gdn_load_frag<3>(a.tf, ch * GDN_BLKS + gdn_low_blk(m, kb)), f, X[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f be = ld4(vec + GDN_V_BETA * 64 + 16 * m + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * m + 4 * g + r;
+                if constexpr (SAVE) {
+                    if (cv && t0 + t < len) a.saved_X[(tv0 + t0 + t) * a.dv + col] = X[m][r];
+                }
+                X[m][r] *= be[r];
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
+#pragma unroll
+            for (int m = 2 * kb; m < 4; ++m)
+                Y[m] = gdn_mm(gdn_load_frag<3>(a.pf, ch * GDN_BLKS + gdn_low_blk(m, kb)), f, Y[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f en = ld4(vec + GDN_V_END * 64 + 16 * m + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = 16 * m + 4 * g + r;
+                if (cv && t0 + t < len) a.y[(tv0 + t0 + t) * a.dv + col] = Y[m][r];
+                X[m][r] *= en[r];
+            }
+        }
+        const float last = vec[GDN_V_GAM * 64 + 63];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) S[d] *= last;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) S[d] = gdn_mm(gdn_load_frag<NT>(a.kt, (ck * DT + d) * 2 + kb), f, S[d]);
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = 16 * d + 4 * g + r;
+            if (cv && row < a.dk) a.stateT[sbase + (size_t)row * a.dv] = S[d][r];
+        }
+}
+
+}  // namespace
+
+GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool backward) {
+    GdnWs w{};
+    const size_t nC = ((size_t)T + GDN_C - 1) / GDN_C;
+    const size_t n = (size_t)B * H * nC, nk = (size_t)B * Hk * nC;
+    const size_t dt = (dk <= 32 ? 2 : dk <= 64 ? 4 : dk <= 128 ? 8 : 16), nt = in_dtype == SDM_DT_F32 ? 3 : 1;
+    size_t o = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = o;
+        o += (bytes + 255) & ~(size_t)255;
+        return at;
+    };
+    w.vec = take(n * GDN_VEC * 64 * 4);
+    w.tf = take(n * GDN_BLKS * 3 * GDN_FRAG * 2);
+    w.pf = take(n * GDN_BLKS * 3 * GDN_FRAG * 2);
+    w.kt = take(nk * dt * 2 * nt * GDN_FRAG * 2);
+    if (backward) {
+        w.qt = take(nk * dt * 2 * nt * GDN_FRAG * 2);
+        w.pm = take(n * 64 * 64 * 4);
+        w.nm = take(n * 64 * 64 * 4);
+        w.dS = take(n * dk * dv * 4);
+    }
+    w.total = o;
+    return w;
+}
+
+#define GDN_PICK_KTN(K)                                  \
+    do {                                                 \
+        if (a.dk <= 32) K(1);                            \
+        else if (a.dk <= 64) K(2);                       \
+        else if (a.dk <= 128) K(4);                      \
+        else K(8);                                       \
+    } while (0)
+
+hipError_t sdm_launch_gdn_step(const GdnArgs& a, hipStream_t st) {
+    const dim3 grid((a.dv + 31) / 32, a.B * a.H);
+#define GDN_STEP(VT)                                                                       \
+    do {                                                                                   \
+        if (a.dk <= 64) gdn_step_kernel<VT, 2><<<grid, 256, 0, st>>>(a);                   \
+        else if (a.dk <= 128) gdn_step_kernel<VT, 4><<<grid, 256, 0, st>>>(a);             \
+        else gdn_step_kernel<VT, 8><<<grid, 256, 0, st>>>(a);                              \
+    } while (0)
+    if (a.in_dtype == SDM_DT_BF16) GDN_STEP(bf16_t);
+    else GDN_STEP(float);
+    return hipGetLastError();
+}
+
+hipError_t sdm_launch_gdn_prep(const GdnArgs& a, bool backward, hipStream_t st) {
+    const dim3 grid(a.nC, a.B * a.H);
+    const bool bf = a.in_dtype == SDM_DT_BF16;
+#define K(N)                                                                                 \
+    do {                                                                                     \
+        if (bf && backward) gdn_prep_kernel<bf16_t, N, true><<<grid, 256, 0, st>>>(a);       \
+        else if (bf) gdn_prep_kernel<bf16_t, N, false><<<grid, 256, 0, st>>>(a);             \
+        else if (backward) gdn_prep_kernel<float, N, true><<<grid, 256, 0, st>>>(a);         \
+        else gdn_prep_kernel<float, N, false><<<grid, 256, 0, st>>>(a);                      \
+    } while (0)
+    GDN_PICK_KTN(K);
+#undef K
+    return hipGetLastError();
+}
+
+hipError_t sdm_launch_gdn_scan(const GdnArgs& a, hipStream_t st) {
+    const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
+    const bool bf = a.in_dtype == SDM_DT_BF16, save = a.saved_S != nullptr;
+#define K(N)                                                                                 \
+    do {                                                                                     \
+        if (bf && save) gdn_scan_kernel<bf16_t, N, true><<<grid, 256, 0, st>>>(a);           \
+        else if (bf) gdn_scan_kernel<bf16_t, N, false><<<grid, 256, 0, st>>>(a);             \
+        else if (save) gdn_scan_kernel<float, N, true><<<grid, 256, 0, st>>>(a);             \
+        else gdn_scan_kernel<float, N, false><<<grid, 256, 0, st>>>(a);                      \
+    } while (0)
+    GDN_PICK_KTN(K);
+#undef K
+    return hipGetLastError();
+}

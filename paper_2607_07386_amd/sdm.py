@@ -9,6 +9,7 @@ call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -74,6 +75,13 @@ def lib() -> ctypes.CDLL:
         for f in ("sdm_scan_fwd_workspace_bytes", "sdm_scan_saved_bytes", "sdm_scan_bwd_workspace_bytes",
                   "sdm_scan_fwd_chunked_workspace_bytes"):
             getattr(L, f).restype = SZ
+        L.sdm_gdn_fwd.argtypes = [P, P, P, I, P, P, P, P, P, I, I, I, I, I, I, P, P, SZ, P, SZ, P]
+        L.sdm_gdn_bwd.argtypes = [P, P, P, I, P, P, P, P, SZ, P, P, I, I, I, I, I, I, P, P, P, P, P, P, P, SZ, P]
+        L.sdm_gdn_fwd_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I]
+        L.sdm_gdn_bwd_workspace_bytes.argtypes = [I, I, I, I, I, I, I]
+        L.sdm_gdn_saved_bytes.argtypes = [I, I, I, I, I]
+        for f in ("sdm_gdn_fwd_workspace_bytes", "sdm_gdn_bwd_workspace_bytes", "sdm_gdn_saved_bytes"):
+            getattr(L, f).restype = SZ
         L.sdm_check_device_errors.argtypes = [P, P]
         L.sdm_profile_enable.argtypes = [I]
         L.sdm_profile_select.argtypes = [ctypes.c_uint]
@@ -88,7 +96,7 @@ def lib() -> ctypes.CDLL:
         L.sdm_version.restype = ctypes.c_char_p
         for f in ("sdm_address", "sdm_scan_fwd", "sdm_scan_fwd_chunked", "sdm_scan_bwd", "sdm_mem_init",
                   "sdm_forward_noalloc", "sdm_gates", "sdm_gates_bwd", "sdm_norm_gate", "sdm_norm_gate_bwd",
-                  "sdm_layer_fwd", "sdm_layer_bwd",
+                  "sdm_layer_fwd", "sdm_layer_bwd", "sdm_gdn_fwd", "sdm_gdn_bwd",
                   "sdm_check_device_errors",
                   "sdm_profile_enable", "sdm_profile_select", "sdm_profile_read"):
             getattr(L, f).restype = I
@@ -598,6 +606,106 @@ def scan_bwd(w_idx, w_val, r_idx, r_val, v, alpha, beta, mem, saved, dy, dmem_T=
     return out
 
 
+def _current(dev):
+    """Context in which `dev` is the current device (launches go to the current one)."""
+    return torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else contextlib.nullcontext()
+
+
+def _check_gdn(q, k, v, alpha, beta, lens):
+    """Shapes and dtypes of the dense rule's inputs; returns (B, Hk, H, T, d_k, d_v)."""
+    _expect_dims(q, "q", 4)
+    _expect_dims(v, "v", 4)
+    B, Hk, T, dk = q.shape
+    H, dv = v.shape[1], v.shape[3]
+    if q.dtype not in _IN:
+        raise TypeError(f"q has dtype {q.dtype}, expected float32 or bfloat16")
+    _expect(k, "k", (B, Hk, T, dk), (q.dtype,))
+    _expect(v, "v", (B, H, T, dv), (q.dtype,))
+    if Hk < 1 or H % Hk:
+        raise ValueError(f"v has {H} heads, not a multiple of q's {Hk}")
+    _expect(alpha, "alpha", (B, H, T), _F32)
+    _expect(beta, "beta", (B, H, T), _F32)
+    if lens is not None:
+        _expect(lens, "lens", (B,), _I32)
+    return B, Hk, H, T, dk, dv
+
+
+def gdn_saved_buffer(B, H, T, d_k, d_v, device) -> torch.Tensor:
+    """What gdn_fwd keeps for gdn_bwd: the states at the chunks' starts and v minus its read-back."""
+    return _ws(lib().sdm_gdn_saved_bytes(B, H, T, d_k, d_v), device)
+
+
+def gdn_fwd_workspace(B, Hk, H, T, d_k, d_v, dtype, device, training=False) -> torch.Tensor:
+    return _ws(lib().sdm_gdn_fwd_workspace_bytes(B, Hk, H, T, d_k, d_v, SDM_BF16 if dtype == torch.bfloat16 else SDM_F32,
+                                                 int(training)), device)
+
+
+def gdn_bwd_workspace(B, Hk, H, T, d_k, d_v, dtype, device) -> torch.Tensor:
+    return _ws(lib().sdm_gdn_bwd_workspace_bytes(B, Hk, H, T, d_k, d_v,
+                                                 SDM_BF16 if dtype == torch.bfloat16 else SDM_F32), device)
+
+
+def gdn_fwd(q, k, v, alpha, beta, state0=None, lens=None, saved=None, workspace=None, y=None, state_out=None):
+    """The dense gated delta rule (Sec. 2, Eq. gdn-update): q, k [B,Hk,T,d_k], v [B,H,T,d_v], alpha, beta
+    [B,H,T] fp32, state0 [B,H,d_k,d_v] fp32 or None (zeros).  lens [B] int32: tokens of each sequence of a
+    padded batch (rows of y past them are zero, or left as they were in a given y).  state_out may be state0
+    (in place).  Returns (y [B,H,T,d_v], state [B,H,d_k,d_v]), fp32."""
+    B, Hk, H, T, dk, dv = _check_gdn(q, k, v, alpha, beta, lens)
+    for t, name in ((state0, "state0"), (state_out, "state_out")):
+        if t is not None:
+            _expect(t, name, (B, H, dk, dv), _F32)
+    if y is not None:
+        _expect(y, "y", (B, H, T, dv), _F32)
+    code = _dtype_code(q)
+    need = lib().sdm_gdn_fwd_workspace_bytes(B, Hk, H, T, dk, dv, code, int(saved is not None))
+    _check_ws(workspace, need)
+    _check_ws(saved, lib().sdm_gdn_saved_bytes(B, H, T, dk, dv), "saved")
+    dev = _dev(q, k, v, alpha, beta, lens, state0, state_out, saved, workspace, y)
+    if y is None:
+        y = (torch.empty if lens is None else torch.zeros)((B, H, T, dv), dtype=torch.float32, device=dev)
+    if state_out is None:
+        state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev)
+    if workspace is None and need:
+        workspace = _ws(need, dev)
+    with _current(dev):
+        rc = lib().sdm_gdn_fwd(_ptr(q), _ptr(k), _ptr(v), code, _ptr(alpha), _ptr(beta), _ptr(lens), _ptr(state0),
+                               _ptr(state_out), B, Hk, H, T, dk, dv, _ptr(y), _ptr(saved),
+                               0 if saved is None else saved.numel(), _ptr(workspace),
+                               0 if workspace is None else workspace.numel(), _stream(dev))
+    _check("sdm_gdn_fwd", rc)
+    return y, state_out
+
+
+def gdn_bwd(q, k, v, alpha, beta, saved, dy, dstate_T=None, lens=None, workspace=None, want_dstate0: bool = True):
+    """Reverse mode of gdn_fwd(..., saved=saved).  Returns a dict of fp32 gradients: dq, dk [B,Hk,T,d_k] (summed
+    over the heads of a key head), dv, dalpha, dbeta and dstate0 (None if not wanted); rows past lens are zero."""
+    B, Hk, H, T, dk_, dv_ = _check_gdn(q, k, v, alpha, beta, lens)
+    _expect(dy, "dy", (B, H, T, dv_), _F32)
+    if dstate_T is not None:
+        _expect(dstate_T, "dstate_T", (B, H, dk_, dv_), _F32)
+    if saved is None:
+        raise ValueError("saved is required")
+    code = _dtype_code(q)
+    need = lib().sdm_gdn_bwd_workspace_bytes(B, Hk, H, T, dk_, dv_, code)
+    _check_ws(workspace, need)
+    _check_ws(saved, lib().sdm_gdn_saved_bytes(B, H, T, dk_, dv_), "saved")
+    dev = _dev(q, k, v, alpha, beta, lens, saved, dy, dstate_T, workspace)
+    new = torch.empty if lens is None else torch.zeros
+    f32 = dict(dtype=torch.float32, device=dev)
+    out = dict(dq=new((B, Hk, T, dk_), **f32), dk=new((B, Hk, T, dk_), **f32), dv=new((B, H, T, dv_), **f32),
+               dalpha=new((B, H, T), **f32), dbeta=new((B, H, T), **f32),
+               dstate0=torch.empty((B, H, dk_, dv_), **f32) if want_dstate0 else None)
+    if workspace is None:
+        workspace = _ws(need, dev)
+    with _current(dev):
+        rc = lib().sdm_gdn_bwd(_ptr(q), _ptr(k), _ptr(v), code, _ptr(alpha), _ptr(beta), _ptr(lens), _ptr(saved),
+                               saved.numel(), _ptr(dy), _ptr(dstate_T), B, Hk, H, T, dk_, dv_, _ptr(out["dq"]),
+                               _ptr(out["dk"]), _ptr(out["dv"]), _ptr(out["dalpha"]), _ptr(out["dbeta"]),
+                               _ptr(out["dstate0"]), _ptr(workspace), workspace.numel(), _stream(dev))
+    _check("sdm_gdn_bwd", rc)
+    return out
+
+
 def mem_init(dst: torch.Tensor, m0: torch.Tensor | None):
     """dst [B,H,N,d_v] = m0 [H,N,d_v] broadcast over B (or zero when m0 is None)."""
     _expect_dims(dst, "dst", 4)
@@ -618,7 +726,7 @@ def check_device_errors(workspace: torch.Tensor):
 
 KERNELS = {"address": 0, "fwd_prep": 1, "fwd_scan": 2, "bwd_prep": 3, "bwd_scan": 4, "bwd_reduce": 5,
            "address_bwd": 6, "mem_init": 7, "decode": 8, "chunk_coef": 9, "chunk_scan": 10, "norm_gate": 11,
-           "gates": 12}
+           "gates": 12, "gdn_prep": 13, "gdn_scan": 14, "gdn_step": 15, "gdn_bwd": 16}
 
 
 def set_chunk_scan_cols(cols: int):
