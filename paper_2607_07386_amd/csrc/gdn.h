@@ -9,12 +9,12 @@
 // products and fp32 x fp32 six; both are cheaper than the fp32 matrix
 // instruction, which runs at 1/16 of the bf16 rate.
 //
-// Layout.  v_mfma_f32_16x16x32_bf16 takes A with row = lane & 15 and eight
-// depths per lane, B with column = lane & 15 likewise, and returns C with
-// column = lane & 15 and rows 4 (lane >> 4) + 0..3.  The order of the 32 depths
-// is free as long as A and B agree; here lane group g = lane >> 4 holds depths
-// 4g .. 4g+3 and 16+4g .. 16+4g+3.  Two stacked C tiles of a product are then a
-// B operand of the next one as they are: a wave chains state, innovations and
+// Layout.  v_mfma_f32_16x16x32_bf16 takes A with row = lane & 15 and depths
+// 8 (lane >> 4) + 0..7, B with column = lane & 15 likewise, and returns C with
+// column = lane & 15 and rows 4 (lane >> 4) + 0..3.  Tiles of 16 rows come in
+// pairs that cover 32 rows, row p of tile m being row gdn_row(m, p) of the matrix:
+// lane group g then holds rows 8g .. 8g+7 of the 32 in its two tiles, which is a
+// B operand of the next product as it is.  A wave chains state, innovations and
 // output without moving a value between lanes.
 #pragma once
 #include "sdm_common.h"
@@ -90,6 +90,9 @@ GDN_DEV int gdn_len(const GdnArgs& a, int b) {
 // upper halves of two words as one word (a in the low half)
 GDN_DEV uint32_t gdn_pack_hi(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
 
+// Row of the matrix that row p of tile m holds (in the C layout p = 4 (lane >> 4) + r).
+GDN_DEV int gdn_row(int m, int p) { return 32 * (m >> 1) + 8 * (p >> 2) + 4 * (m & 1) + (p & 3); }
+
 // Eight fp32 values as three bf16 parts, x = t0 + t1 + t2 up to 2^-24 |x|: each part
 // is the top 16 bits of what the parts before it leave (the differences are exact).
 GDN_DEV GdnFrag<3> gdn_split(const float (&x)[8]) {
@@ -141,9 +144,9 @@ GDN_DEV sdm_f32x4 gdn_mm(const GdnFrag<NA>& a, const GdnFrag<NB>& b, sdm_f32x4 c
 // Depth block kb of one row of `n` values (n % 4 == 0; zeros past the end or where
 // the row is none) in this lane group's depths.
 GDN_DEV void gdn_row8(const float* row, int kb, int n, bool ok, float (&x)[8]) {
-    const int p = 32 * kb + 4 * (lane_id() >> 4);
+    const int p = 32 * kb + 8 * (lane_id() >> 4);
     const v4f a = ok && p < n ? ld4(row + p) : v4zero();
-    const v4f b = ok && p + 16 < n ? ld4(row + p + 16) : v4zero();
+    const v4f b = ok && p + 4 < n ? ld4(row + p + 4) : v4zero();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[i] = a[i];
@@ -158,13 +161,13 @@ GDN_DEV GdnFrag<NT> gdn_row_frag(const float* row, int kb, int n, bool ok) {
 }
 template <int NT>
 GDN_DEV GdnFrag<NT> gdn_row_frag(const bf16_t* row, int kb, int n, bool ok) {
-    const int p = 32 * kb + 4 * (lane_id() >> 4);
+    const int p = 32 * kb + 8 * (lane_id() >> 4);
     union {
         u2v u[2];
         sdm_bf16x8 v;
     } f;
     f.u[0] = ok && p < n ? *reinterpret_cast<const u2v*>(row + p) : u2v{0u, 0u};
-    f.u[1] = ok && p + 16 < n ? *reinterpret_cast<const u2v*>(row + p + 16) : u2v{0u, 0u};
+    f.u[1] = ok && p + 4 < n ? *reinterpret_cast<const u2v*>(row + p + 4) : u2v{0u, 0u};
     GdnFrag<NT> r;
     r.t[0] = f.v;
     return r;
@@ -195,6 +198,44 @@ template <>
 struct GdnIn<bf16_t> {
     static constexpr int NT = 1;
 };
+
+// ---- staging of fragments: memory -> registers (a chunk ahead) -> LDS ----
+// N fragments of this wave, `first` on, from fragments as the prep kernel laid
+// them out; a fragment is 1 KB, 16 bytes a lane.
+template <int N>
+GDN_DEV void gdn_fetch(u4v (&r)[N], const uint16_t* base, int first) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u4v*>(base + (size_t)(first + i) * GDN_FRAG + lane_id() * 8);
+}
+// The fragments (m, 0 .. N-1) of 16 rows of a bf16 matrix (row length n, n % 4 == 0):
+// lane row gdn_row(m, lane & 15).  Rows from `rows` on repeat the last one (what
+// they give is masked where it is used); depths past n are zero.
+template <int N>
+GDN_DEV void gdn_fetch_rows(u4v (&r)[N], const bf16_t* base, int m, int rows, int n) {
+    const int row = min(gdn_row(m, lane_id() & 15), rows - 1), p0 = 8 * (lane_id() >> 4);
+    const bf16_t* src = base + (size_t)row * n;
+    if (n % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = 32 * i + p0;
+            r[i] = *reinterpret_cast<const u4v*>(src + (p < n ? p : 0));
+            if (p >= n) r[i] = u4v{0u, 0u, 0u, 0u};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = 32 * i + p0;
+            const u2v lo = p < n ? *reinterpret_cast<const u2v*>(src + p) : u2v{0u, 0u};
+            const u2v hi = p + 4 < n ? *reinterpret_cast<const u2v*>(src + p + 4) : u2v{0u, 0u};
+            r[i] = u4v{lo.x, lo.y, hi.x, hi.y};
+        }
+    }
+}
+template <int N>
+GDN_DEV void gdn_stage(uint16_t* lds, int first, const u4v (&r)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<u4v*>(lds + (first + i) * GDN_FRAG + lane_id() * 8) = r[i];
+}
 
 // exp(lambda_i - lambda_j), the sums of log alpha held as two floats each (a
 // difference of two long sums keeps its digits)

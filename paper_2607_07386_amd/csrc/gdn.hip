@@ -272,7 +272,7 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
         float x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int rr = 16 * mt + r16, cc = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+            const int rr = gdn_row(mt, r16), cc = 32 * kb + 8 * g + i;
             x[i] = BWD ? src[cc * LD + rr] : src[rr * LD + cc];
         }
         gdn_store_frag<3>(f < GDN_BLKS ? a.tf : a.pf, ch * GDN_BLKS + blk, gdn_split(x));
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
         for (int f = w; f < (BWD ? 2 : 1) * DT * 2; f += 4) {
             const int id = f % (DT * 2), dt = id >> 1, kb = id & 1;
             const VT* src = f < DT * 2 ? kp : qp;
-            const int d = 16 * dt + r16;
+            const int d = gdn_row(dt, r16);
             GdnFrag<NT> fr;
             if constexpr (NT == 1) {
                 union {
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
                 } x;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int t = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+                    const int t = 32 * kb + 8 * g + i;
                     x.u[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d].bits : (uint16_t)0;
                 }
                 fr.t[0] = x.v;
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
                 float x[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const int t = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+                    const int t = 32 * kb + 8 * g + i;
                     x[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d] : 0.f;
                 }
                 fr = gdn_split(x);
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int row = 16 * d + 4 * g + r;
+            const int row = gdn_row(d, 4 * g + r);
             S[d][r] = a.state0 && cv && row < a.dk ? a.state0[sbase + (size_t)row * a.dv] : 0.f;
         }
     const size_t tq0 = (size_t)(b * a.Hk + hk) * a.T, tv0 = (size_t)bh * a.T;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = 16 * d + 4 * g + r;
+                    const int row = gdn_row(d, 4 * g + r);
                     if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
                 }
         }
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
             const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
-                const int row = 16 * m + r16;
+                const int row = gdn_row(m, r16);
                 const bool ok = t0 + row < len;
                 R[m] = gdn_mm(gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, ok), s, R[m]);
                 Y[m] = gdn_mm(gdn_row_frag<NT>(qp + (size_t)row * a.dk, kb, a.dk, ok), s, Y[m]);
@@ -372,10 +372,10 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const v4f gam = ld4(vec + GDN_V_GAM * 64 + 16 * m + 4 * g);
+            const v4f gam = ld4(vec + GDN_V_GAM * 64 + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g + r;
+                const int t = gdn_row(m, 4 * g + r);
                 const float v = cv && t0 + t < len ? to_f32(vp[(size_t)t * a.dv]) : 0.f;
                 R[m][r] = fmaf(-gam[r], R[m][r], v);
                 Y[m][r] *= gam[r];
@@ -393,10 +393,10 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const v4f be = ld4(vec + GDN_V_BETA * 64 + 16 * m + 4 * g);
+            const v4f be = ld4(vec + GDN_V_BETA * 64 + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g + r;
+                const int t = gdn_row(m, 4 * g + r);
                 if constexpr (SAVE) {
                     if (cv && t0 + t < len) a.saved_X[(tv0 + t0 + t) * a.dv + col] = X[m][r];
                 }
@@ -412,10 +412,10 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const v4f en = ld4(vec + GDN_V_END * 64 + 16 * m + 4 * g);
+            const v4f en = ld4(vec + GDN_V_END * 64 + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g + r;
+                const int t = gdn_row(m, 4 * g + r);
                 if (cv && t0 + t < len) a.y[(tv0 + t0 + t) * a.dv + col] = Y[m][r];
                 X[m][r] *= en[r];
             }
@@ -434,9 +434,210 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int row = 16 * d + 4 * g + r;
+            const int row = gdn_row(d, 4 * g + r);
             if (cv && row < a.dk) a.stateT[sbase + (size_t)row * a.dv] = S[d][r];
         }
+}
+
+// The same walk for bf16 inputs with the chunk's fragments staged in LDS, one copy
+// for the workgroup's four waves, each piece fetched into registers a chunk ahead
+// and written over the last one as soon as every wave is done with it.
+template <int KTN>
+constexpr size_t scan_lds() {
+    return (size_t)(12 * KTN + 36) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+}
+
+template <int KTN, bool SAVE>
+__global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
+    constexpr int DT = 2 * KTN;
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // K [4][KTN], then Q
+    uint16_t* sQ = sK + 4 * KTN * GDN_FRAG;
+    uint16_t* sT = sQ + 4 * KTN * GDN_FRAG;                 // T' [6][3], then P
+    uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;
+    uint16_t* sKT = sP + GDN_BLKS * 3 * GDN_FRAG;           // K^T [DT][2]
+    float* sV = reinterpret_cast<float*>(sKT + 4 * KTN * GDN_FRAG);   // [2][gamma, end, beta][64]
+
+    const int groups = (a.dv + 63) / 64;
+    int grp, bh;
+    scan_wg_coords<true>(groups, grp, bh);
+    const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
+    const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
+    const int tid = threadIdx.x, w = tid >> 6, lane = lane_id(), r16 = lane & 15, g = lane >> 4;
+    const int col = (grp * 4 + w) * 16 + r16;
+    const bool cv = col < a.dv;
+    const size_t sbase = (size_t)bh * a.dk * a.dv + (cv ? col : 0);
+    const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    sdm_f32x4 S[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = gdn_row(d, 4 * g + r);
+            S[d][r] = a.state0 && cv && row < a.dk ? a.state0[sbase + (size_t)row * a.dv] : 0.f;
+        }
+    const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const bf16_t* vp = static_cast<const bf16_t*>(a.v) + (size_t)bh * a.T * a.dv + (cv ? col : 0);
+    float* yp = a.y + (size_t)bh * a.T * a.dv + col;
+    const size_t ch0 = (size_t)bh * a.nC, ck0 = (size_t)(b * a.Hk + hk) * a.nC;
+
+    u4v rK[KTN], rQ[KTN], rT[9], rKT[KTN];
+    float rV, V[4][4];
+    const auto fetch_kq = [&](int c) {
+        const int t0 = c * GDN_C;
+        gdn_fetch_rows(rK, kp + (size_t)t0 * a.dk, w, len - t0, a.dk);
+        gdn_fetch_rows(rQ, qp + (size_t)t0 * a.dk, w, len - t0, a.dk);
+        const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // wave 3 repeats wave 2
+        rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
+    };
+    const auto fetch_v = [&](int c) {
+        const int t0 = c * GDN_C;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                V[m][r] = to_f32(vp[(size_t)min(t0 + gdn_row(m, 4 * g + r), len - 1) * a.dv]);
+    };
+    const auto fetch_t = [&](int c) {   // 18 fragments of T' (waves 0, 1), 18 of P
+        const uint16_t* src = w < 2 ? a.tf : a.pf;
+        gdn_fetch(rT, src + (ch0 + c) * GDN_BLKS * 3 * GDN_FRAG, (w & 1) * 9);
+    };
+    const auto fetch_kt = [&](int c) { gdn_fetch(rKT, a.kt + (ck0 + c) * DT * 2 * GDN_FRAG, w * KTN); };
+    const auto stage_kq = [&](int par) {
+        gdn_stage(sK, w * KTN, rK);
+        gdn_stage(sQ, w * KTN, rQ);
+        if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
+    };
+    const auto stage_t = [&]() { gdn_stage(sT, w * 9, rT); };
+    const auto stage_kt = [&]() { gdn_stage(sKT, w * KTN, rKT); };
+
+    if (nc > 0) {
+        fetch_kq(0);
+        fetch_v(0);
+        fetch_t(0);
+        fetch_kt(0);
+        stage_kq(0);
+        stage_t();
+        stage_kt();
+        const int c1 = min(1, nc - 1);
+        fetch_kq(c1);
+        fetch_t(c1);
+        fetch_kt(c1);
+        __syncthreads();
+    }
+    for (int c = 0; c < nc; ++c) {
+        const int t0 = c * GDN_C, left = len - t0, next = min(c + 2, nc - 1);
+        const float* vec = sV + (c & 1) * 3 * 64;
+        if constexpr (SAVE) {
+            float* o = a.saved_S + (ch0 + c) * a.dk * a.dv + col;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = gdn_row(d, 4 * g + r);
+                    if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
+                }
+        }
+        sdm_f32x4 R[4], Y[4], X[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) R[m] = Y[m] = X[m] = zero;
+#pragma unroll
+        for (int kb = 0; kb < KTN; ++kb) {
+            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) R[m] = gdn_mm(gdn_load_frag<1>(sK, m * KTN + kb), s, R[m]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) Y[m] = gdn_mm(gdn_load_frag<1>(sQ, m * KTN + kb), s, Y[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f gam = ld4(vec + gdn_row(m, 4 * g));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const bool on = gdn_row(m, 4 * g + r) < left;
+                R[m][r] = on ? fmaf(-gam[r], R[m][r], V[m][r]) : 0.f;
+                Y[m][r] *= gam[r];
+            }
+        }
+        __syncthreads();
+        if (c + 1 < nc) {
+            stage_kq((c + 1) & 1);
+            fetch_v(c + 1);
+            fetch_kq(next);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(R[2 * kb], R[2 * kb + 1]);
+#pragma unroll
+            for (int m = 2 * kb; m < 4; ++m) X[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_low_blk(m, kb)), f, X[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f be = ld4(vec + 128 + gdn_row(m, 4 * g));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = gdn_row(m, 4 * g + r);
+                if constexpr (SAVE) {
+                    if (cv && t < left) a.saved_X[((size_t)bh * a.T + t0 + t) * a.dv + col] = X[m][r];
+                }
+                X[m][r] *= be[r];
+            }
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
+#pragma unroll
+            for (int m = 2 * kb; m < 4; ++m) Y[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_low_blk(m, kb)), f, Y[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f en = ld4(vec + 64 + gdn_row(m, 4 * g));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = gdn_row(m, 4 * g + r);
+                if (cv && t < left) yp[(size_t)(t0 + t) * a.dv] = Y[m][r];
+                X[m][r] *= en[r];
+            }
+        }
+        const float last = vec[63];
+        __syncthreads();
+        if (c + 1 < nc) {
+            stage_t();
+            fetch_t(next);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) S[d] *= last;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) S[d] = gdn_mm(gdn_load_frag<1>(sKT, d * 2 + kb), f, S[d]);
+        }
+        __syncthreads();
+        if (c + 1 < nc) {
+            stage_kt();
+            fetch_kt(next);
+        }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = gdn_row(d, 4 * g + r);
+            if (cv && row < a.dk) a.stateT[sbase + (size_t)row * a.dv] = S[d][r];
+        }
+}
+
+template <int KTN, bool SAVE>
+hipError_t launch_scan_staged(const GdnArgs& a, hipStream_t st) {
+    const auto kfn = gdn_scan_staged_kernel<KTN, SAVE>;
+    constexpr size_t lds = scan_lds<KTN>();
+    hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    kfn<<<dim3((a.dv + 63) / 64 * a.B * a.H), 256, lds, st>>>(a);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -507,8 +708,8 @@ hipError_t sdm_launch_gdn_scan(const GdnArgs& a, hipStream_t st) {
     const bool bf = a.in_dtype == SDM_DT_BF16, save = a.saved_S != nullptr;
 #define K(N)                                                                                 \
     do {                                                                                     \
-        if (bf && save) gdn_scan_kernel<bf16_t, N, true><<<grid, 256, 0, st>>>(a);           \
-        else if (bf) gdn_scan_kernel<bf16_t, N, false><<<grid, 256, 0, st>>>(a);             \
+        if (bf && save) return launch_scan_staged<N, true>(a, st);                           \
+        else if (bf) return launch_scan_staged<N, false>(a, st);                             \
         else if (save) gdn_scan_kernel<float, N, true><<<grid, 256, 0, st>>>(a);             \
         else gdn_scan_kernel<float, N, false><<<grid, 256, 0, st>>>(a);                      \
     } while (0)

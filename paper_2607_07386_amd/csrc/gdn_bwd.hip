@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int row = 16 * d + 4 * g + r;
+            const int row = gdn_row(d, 4 * g + r);
             S[d][r] = a.dstateT && cv && row < a.dk ? a.dstateT[sbase + (size_t)row * a.dv] : 0.f;
         }
     const size_t tq0 = (size_t)(b * a.Hk + hk) * a.T, tv0 = (size_t)bh * a.T;
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int row = 16 * d + 4 * g + r;
+                const int row = gdn_row(d, 4 * g + r);
                 if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
             }
         sdm_f32x4 dE[4], Y[4];
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
             dE[m] = zero;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g + r;
+                const int t = gdn_row(m, 4 * g + r);
                 Y[m][r] = cv && t0 + t < len ? a.dy[(tv0 + t0 + t) * a.dv + col] : 0.f;
             }
         }
@@ -75,13 +75,13 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
             const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
-                const int row = 16 * m + r16;
+                const int row = gdn_row(m, r16);
                 dE[m] = gdn_mm(gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, t0 + row < len), s, dE[m]);
             }
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const v4f en = ld4(vec + GDN_V_END * 64 + 16 * m + 4 * g);
+            const v4f en = ld4(vec + GDN_V_END * 64 + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) dE[m][r] *= en[r];
         }
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const v4f be = ld4(vec + GDN_V_BETA * 64 + 16 * m + 4 * g);
+            const v4f be = ld4(vec + GDN_V_BETA * 64 + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) dE[m][r] *= be[r];
         }
@@ -110,10 +110,10 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
         }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            const v4f gam = ld4(vec + GDN_V_GAM * 64 + 16 * m + 4 * g);
+            const v4f gam = ld4(vec + GDN_V_GAM * 64 + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = 16 * m + 4 * g + r;
+                const int t = gdn_row(m, 4 * g + r);
                 if (cv && t0 + t < len) a.dvv[(tv0 + t0 + t) * a.dv + col] = dR[m][r];
                 dR[m][r] *= -gam[r];
                 Y[m][r] *= gam[r];
@@ -138,10 +138,202 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int row = 16 * d + 4 * g + r;
+                const int row = gdn_row(d, 4 * g + r);
                 if (cv && row < a.dk) a.dstate0[sbase + (size_t)row * a.dv] = S[d][r];
             }
     }
+}
+
+// The same walk for bf16 inputs, fragments staged in LDS as in the forward scan.
+template <int KTN>
+__global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
+    constexpr int DT = 2 * KTN;
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // K [4][KTN]
+    uint16_t* sT = sK + 4 * KTN * GDN_FRAG;                 // T'^T [6][3], then P^T
+    uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;
+    uint16_t* sKT = sP + GDN_BLKS * 3 * GDN_FRAG;           // K^T [DT][2], then Q^T
+    uint16_t* sQT = sKT + 4 * KTN * GDN_FRAG;
+    float* sV = reinterpret_cast<float*>(sQT + 4 * KTN * GDN_FRAG);   // [2][gamma, end, beta][64]
+
+    const int groups = (a.dv + 63) / 64;
+    int grp, bh;
+    scan_wg_coords<true>(groups, grp, bh);
+    const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
+    const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
+    const int tid = threadIdx.x, w = tid >> 6, lane = lane_id(), r16 = lane & 15, g = lane >> 4;
+    const int col = (grp * 4 + w) * 16 + r16;
+    const bool cv = col < a.dv;
+    const size_t sbase = (size_t)bh * a.dk * a.dv + (cv ? col : 0);
+    const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+    sdm_f32x4 S[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = gdn_row(d, 4 * g + r);
+            S[d][r] = a.dstateT && cv && row < a.dk ? a.dstateT[sbase + (size_t)row * a.dv] : 0.f;
+        }
+    const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const float* yp = a.dy + (size_t)bh * a.T * a.dv + (cv ? col : 0);
+    float* dvp = a.dvv + (size_t)bh * a.T * a.dv + col;
+    const size_t ch0 = (size_t)bh * a.nC, ck0 = (size_t)(b * a.Hk + hk) * a.nC;
+
+    u4v rK[KTN], rT[9], rKT[KTN], rQT[KTN];
+    float rV, rY[4][4];
+    const auto fetch_k = [&](int c) {
+        gdn_fetch_rows(rK, kp + (size_t)c * GDN_C * a.dk, w, len - c * GDN_C, a.dk);
+        const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // wave 3 repeats wave 2
+        rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
+    };
+    const auto fetch_y = [&](int c) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                rY[m][r] = yp[(size_t)min(c * GDN_C + gdn_row(m, 4 * g + r), len - 1) * a.dv];
+    };
+    const auto fetch_t = [&](int c) {
+        const uint16_t* src = w < 2 ? a.tf : a.pf;
+        gdn_fetch(rT, src + (ch0 + c) * GDN_BLKS * 3 * GDN_FRAG, (w & 1) * 9);
+    };
+    const auto fetch_kt = [&](int c) {
+        gdn_fetch(rKT, a.kt + (ck0 + c) * DT * 2 * GDN_FRAG, w * KTN);
+        gdn_fetch(rQT, a.qt + (ck0 + c) * DT * 2 * GDN_FRAG, w * KTN);
+    };
+    const auto stage_k = [&](int par) {
+        gdn_stage(sK, w * KTN, rK);
+        if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
+    };
+    const auto stage_t = [&]() { gdn_stage(sT, w * 9, rT); };
+    const auto stage_kt = [&]() {
+        gdn_stage(sKT, w * KTN, rKT);
+        gdn_stage(sQT, w * KTN, rQT);
+    };
+
+    if (nc > 0) {
+        fetch_k(nc - 1);
+        fetch_y(nc - 1);
+        fetch_t(nc - 1);
+        fetch_kt(nc - 1);
+        stage_k((nc - 1) & 1);
+        stage_t();
+        stage_kt();
+        const int c1 = max(nc - 2, 0);
+        fetch_k(c1);
+        fetch_t(c1);
+        fetch_kt(c1);
+        __syncthreads();
+    }
+    for (int c = nc - 1; c >= 0; --c) {
+        const int t0 = c * GDN_C, left = len - t0, next = max(c - 2, 0);
+        const float* vec = sV + (c & 1) * 3 * 64;
+        float* o = a.dS + (ch0 + c) * a.dk * a.dv + col;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = gdn_row(d, 4 * g + r);
+                if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
+            }
+        sdm_f32x4 dE[4], Y[4], dR[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            dE[m] = dR[m] = zero;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) Y[m][r] = gdn_row(m, 4 * g + r) < left ? rY[m][r] : 0.f;
+        }
+#pragma unroll
+        for (int kb = 0; kb < KTN; ++kb) {
+            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) dE[m] = gdn_mm(gdn_load_frag<1>(sK, m * KTN + kb), s, dE[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f en = ld4(vec + 64 + gdn_row(m, 4 * g));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dE[m][r] *= gdn_row(m, 4 * g + r) < left ? en[r] : 0.f;
+        }
+        __syncthreads();
+        if (c > 0) {
+            stage_k((c - 1) & 1);
+            fetch_y(c - 1);
+            fetch_k(next);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
+#pragma unroll
+            for (int m = 0; m < 2 * kb + 2; ++m) dE[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_up_blk(m, kb)), f, dE[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f be = ld4(vec + 128 + gdn_row(m, 4 * g));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dE[m][r] *= be[r];
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> f = gdn_stack(dE[2 * kb], dE[2 * kb + 1]);
+#pragma unroll
+            for (int m = 0; m < 2 * kb + 2; ++m) dR[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_up_blk(m, kb)), f, dR[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const v4f gam = ld4(vec + gdn_row(m, 4 * g));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int t = gdn_row(m, 4 * g + r);
+                if (cv && t < left) dvp[(size_t)(t0 + t) * a.dv] = dR[m][r];
+                dR[m][r] *= -gam[r];
+                Y[m][r] *= gam[r];
+            }
+        }
+        const float last = vec[63];
+        __syncthreads();
+        if (c > 0) {
+            stage_t();
+            fetch_t(next);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) S[d] *= last;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const GdnFrag<3> fr = gdn_stack(dR[2 * kb], dR[2 * kb + 1]);
+            const GdnFrag<3> fy = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                S[d] = gdn_mm(gdn_load_frag<1>(sKT, d * 2 + kb), fr, S[d]);
+                S[d] = gdn_mm(gdn_load_frag<1>(sQT, d * 2 + kb), fy, S[d]);
+            }
+        }
+        __syncthreads();
+        if (c > 0) {
+            stage_kt();
+            fetch_kt(next);
+        }
+    }
+    if (a.dstate0) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = gdn_row(d, 4 * g + r);
+                if (cv && row < a.dk) a.dstate0[sbase + (size_t)row * a.dv] = S[d][r];
+            }
+    }
+}
+
+template <int KTN>
+hipError_t launch_adjoint_staged(const GdnArgs& a, hipStream_t st) {
+    const auto kfn = gdn_adjoint_staged_kernel<KTN>;
+    constexpr size_t lds = (size_t)(12 * KTN + 36) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+    hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    kfn<<<dim3((a.dv + 63) / 64 * a.B * a.H), 256, lds, st>>>(a);
+    return hipGetLastError();
 }
 
 // ---------------------------------------------------------------- gradients
@@ -213,7 +405,7 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
             const GdnFrag<3> fr = gdn_row_frag<3>(rr, kb, a.dv, aok);
             gdn_store_frag<3>(sX, w, fx);
             for (int d = w; d < DT; d += 4) {
-                const int row = 16 * d + r16;
+                const int row = gdn_row(d, r16);
                 float x0[8], x1[8];
                 gdn_row8(S0 + (size_t)row * a.dv, kb, a.dv, row < a.dk, x0);
                 gdn_row8(S1 + (size_t)row * a.dv, kb, a.dv, row < a.dk, x1);
@@ -253,7 +445,7 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
         }
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-            const int dc = 16 * d + r16;
+            const int dc = gdn_row(d, r16);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int i = 16 * w + 4 * g + r;
@@ -357,7 +549,7 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
             float xp[8], xt[8], xn[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int j = 32 * kb + 4 * g + (i & 3) + 16 * (i >> 2);
+                const int j = 32 * kb + 8 * g + i;
                 xp[i] = mP[arow * LD + j];
                 xt[i] = mP[j * LD + arow];
                 xn[i] = -(mN[arow * LD + j] + mN[j * LD + arow]);
@@ -375,7 +567,7 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
     }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-        const int dc = 16 * d + r16;
+        const int dc = gdn_row(d, r16);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * w + 4 * g + r;
@@ -412,7 +604,7 @@ hipError_t sdm_launch_gdn_adjoint(const GdnArgs& a, hipStream_t st) {
     const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
 #define F(N)                                                                                 \
     do {                                                                                     \
-        if (a.in_dtype == SDM_DT_BF16) gdn_adjoint_kernel<bf16_t, N><<<grid, 256, 0, st>>>(a); \
+        if (a.in_dtype == SDM_DT_BF16) return launch_adjoint_staged<N>(a, st);               \
         else gdn_adjoint_kernel<float, N><<<grid, 256, 0, st>>>(a);                          \
     } while (0)
     GDN_PICK(F);
