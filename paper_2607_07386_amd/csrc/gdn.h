@@ -84,7 +84,7 @@ struct GdnFrag {
 GDN_DEV int gdn_len(const GdnArgs& a, int b) {
     if (!a.lens) return a.T;
     const int n = a.lens[b];
-    return n < 0 ? 0 : (n > a.T ? a.T : n);
+    return __builtin_amdgcn_readfirstlane(n < 0 ? 0 : (n > a.T ? a.T : n));   // one value for the workgroup
 }
 
 // upper halves of two words as one word (a in the low half)
@@ -207,29 +207,59 @@ GDN_DEV void gdn_fetch(u4v (&r)[N], const uint16_t* base, int first) {
 #pragma unroll
     for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u4v*>(base + (size_t)(first + i) * GDN_FRAG + lane_id() * 8);
 }
-// The fragments (m, 0 .. N-1) of 16 rows of a bf16 matrix (row length n, n % 4 == 0):
-// lane row gdn_row(m, lane & 15).  Rows from `rows` on repeat the last one (what
-// they give is masked where it is used); depths past n are zero.
+// Buffers of one chunk or one state: a load past `bytes` gives zeros and a store there
+// does nothing, so rows past a sequence's end and past d_k need no branch (a branch
+// around a store makes the compiler wait for every load in flight at the next use).
+// Columns past d_v take GDN_OUT for their offset.
+#define GDN_OUT 0x40000000u
+GDN_DEV __amdgpu_buffer_rsrc_t gdn_buf(const void* p, size_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
+}
+GDN_DEV float gdn_ldf(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)off, 0, 0));
+}
+GDN_DEV void gdn_stf(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, (int)off, 0, 0);
+}
+// The fragments (m, 0 .. N-1) of 16 rows of a bf16 matrix of `rows` rows of n values
+// (n % 4 == 0): lane row gdn_row(m, lane & 15).  Rows and depths past the end are zero.
 template <int N>
 GDN_DEV void gdn_fetch_rows(u4v (&r)[N], const bf16_t* base, int m, int rows, int n) {
-    const int row = min(gdn_row(m, lane_id() & 15), rows - 1), p0 = 8 * (lane_id() >> 4);
-    const bf16_t* src = base + (size_t)row * n;
+    const auto buf = gdn_buf(base, (size_t)min(rows, GDN_C) * n * 2);
+    const uint32_t row = gdn_row(m, lane_id() & 15) * n * 2;
+    const int p0 = 8 * (lane_id() >> 4);
     if (n % 8 == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int p = 32 * i + p0;
-            r[i] = *reinterpret_cast<const u4v*>(src + (p < n ? p : 0));
-            if (p >= n) r[i] = u4v{0u, 0u, 0u, 0u};
+            r[i] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(buf, (int)(p < n ? row + p * 2 : GDN_OUT), 0, 0));
         }
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int p = 32 * i + p0;
-            const u2v lo = p < n ? *reinterpret_cast<const u2v*>(src + p) : u2v{0u, 0u};
-            const u2v hi = p + 4 < n ? *reinterpret_cast<const u2v*>(src + p + 4) : u2v{0u, 0u};
+            const u2v lo = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p < n ? row + p * 2 : GDN_OUT), 0, 0));
+            const u2v hi = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p + 4 < n ? row + p * 2 + 8 : GDN_OUT), 0, 0));
             r[i] = u4v{lo.x, lo.y, hi.x, hi.y};
         }
     }
+}
+// A state's 16 columns of this lane's column offset `co` (bytes) in the C layout.
+template <int DT>
+GDN_DEV void gdn_load_state(sdm_f32x4 (&S)[DT], const float* p, int dk, int dv, uint32_t co) {
+    const auto buf = gdn_buf(p, p ? (size_t)dk * dv * 4 : 0);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[d][r] = gdn_ldf(buf, gdn_row(d, 4 * (lane_id() >> 4) + r) * dv * 4 + co);
+}
+template <int DT>
+GDN_DEV void gdn_store_state(const sdm_f32x4 (&S)[DT], float* p, int dk, int dv, uint32_t co) {
+    const auto buf = gdn_buf(p, (size_t)dk * dv * 4);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) gdn_stf(buf, gdn_row(d, 4 * (lane_id() >> 4) + r) * dv * 4 + co, S[d][r]);
 }
 template <int N>
 GDN_DEV void gdn_stage(uint16_t* lds, int first, const u4v (&r)[N]) {

@@ -463,24 +463,18 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
     scan_wg_coords<true>(groups, grp, bh);
     const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
     const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
-    const int tid = threadIdx.x, w = tid >> 6, lane = lane_id(), r16 = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), r16 = lane & 15, g = lane >> 4;
     const int col = (grp * 4 + w) * 16 + r16;
     const bool cv = col < a.dv;
-    const size_t sbase = (size_t)bh * a.dk * a.dv + (cv ? col : 0);
+    const uint32_t co = cv ? col * 4 : GDN_OUT, co2 = cv ? col * 2 : GDN_OUT;   // column offsets: fp32, bf16
+    const size_t sn = (size_t)a.dk * a.dv;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     sdm_f32x4 S[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = gdn_row(d, 4 * g + r);
-            S[d][r] = a.state0 && cv && row < a.dk ? a.state0[sbase + (size_t)row * a.dv] : 0.f;
-        }
+    gdn_load_state(S, a.state0 ? a.state0 + bh * sn : nullptr, a.dk, a.dv, co);
     const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
     const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
-    const bf16_t* vp = static_cast<const bf16_t*>(a.v) + (size_t)bh * a.T * a.dv + (cv ? col : 0);
-    float* yp = a.y + (size_t)bh * a.T * a.dv + col;
+    const bf16_t* vp = static_cast<const bf16_t*>(a.v) + (size_t)bh * a.T * a.dv;
     const size_t ch0 = (size_t)bh * a.nC, ck0 = (size_t)(b * a.Hk + hk) * a.nC;
 
     u4v rK[KTN], rQ[KTN], rT[9], rKT[KTN];
@@ -494,11 +488,13 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
     };
     const auto fetch_v = [&](int c) {
         const int t0 = c * GDN_C;
+        const auto buf = gdn_buf(vp + (size_t)t0 * a.dv, (size_t)min(len - t0, GDN_C) * a.dv * 2);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                V[m][r] = to_f32(vp[(size_t)min(t0 + gdn_row(m, 4 * g + r), len - 1) * a.dv]);
+                V[m][r] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b16(
+                                              buf, (int)(gdn_row(m, 4 * g + r) * a.dv * 2 + co2), 0, 0) << 16);
     };
     const auto fetch_t = [&](int c) {   // 18 fragments of T' (waves 0, 1), 18 of P
         const uint16_t* src = w < 2 ? a.tf : a.pf;
@@ -527,19 +523,15 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
         fetch_kt(c1);
         __syncthreads();
     }
+    // (the last chunks fetch and stage once more what nobody reads: without the
+    // branches the compiler counts the loads in flight across the loop)
     for (int c = 0; c < nc; ++c) {
         const int t0 = c * GDN_C, left = len - t0, next = min(c + 2, nc - 1);
         const float* vec = sV + (c & 1) * 3 * 64;
-        if constexpr (SAVE) {
-            float* o = a.saved_S + (ch0 + c) * a.dk * a.dv + col;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = gdn_row(d, 4 * g + r);
-                    if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
-                }
-        }
+        const auto ybuf = gdn_buf(a.y + ((size_t)bh * a.T + t0) * a.dv, (size_t)min(left, GDN_C) * a.dv * 4);
+        const auto xbuf = gdn_buf(SAVE ? a.saved_X + ((size_t)bh * a.T + t0) * a.dv : nullptr,
+                                  (size_t)min(left, GDN_C) * a.dv * 4);
+        if constexpr (SAVE) gdn_store_state(S, a.saved_S + (ch0 + c) * sn, a.dk, a.dv, co);
         sdm_f32x4 R[4], Y[4], X[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) R[m] = Y[m] = X[m] = zero;
@@ -556,17 +548,14 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
             const v4f gam = ld4(vec + gdn_row(m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const bool on = gdn_row(m, 4 * g + r) < left;
-                R[m][r] = on ? fmaf(-gam[r], R[m][r], V[m][r]) : 0.f;
+                R[m][r] = fmaf(-gam[r], R[m][r], V[m][r]);   // 0 past the end: K and V are
                 Y[m][r] *= gam[r];
             }
         }
         __syncthreads();
-        if (c + 1 < nc) {
-            stage_kq((c + 1) & 1);
-            fetch_v(c + 1);
-            fetch_kq(next);
-        }
+        stage_kq((c + 1) & 1);
+        fetch_v(min(c + 1, nc - 1));
+        fetch_kq(next);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const GdnFrag<3> f = gdn_stack(R[2 * kb], R[2 * kb + 1]);
@@ -579,9 +568,7 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = gdn_row(m, 4 * g + r);
-                if constexpr (SAVE) {
-                    if (cv && t < left) a.saved_X[((size_t)bh * a.T + t0 + t) * a.dv + col] = X[m][r];
-                }
+                if constexpr (SAVE) gdn_stf(xbuf, t * a.dv * 4 + co, X[m][r]);
                 X[m][r] *= be[r];
             }
         }
@@ -597,16 +584,14 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = gdn_row(m, 4 * g + r);
-                if (cv && t < left) yp[(size_t)(t0 + t) * a.dv] = Y[m][r];
+                gdn_stf(ybuf, t * a.dv * 4 + co, Y[m][r]);
                 X[m][r] *= en[r];
             }
         }
         const float last = vec[63];
         __syncthreads();
-        if (c + 1 < nc) {
-            stage_t();
-            fetch_t(next);
-        }
+        stage_t();
+        fetch_t(next);
 #pragma unroll
         for (int d = 0; d < DT; ++d) S[d] *= last;
 #pragma unroll
@@ -616,18 +601,10 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
             for (int d = 0; d < DT; ++d) S[d] = gdn_mm(gdn_load_frag<1>(sKT, d * 2 + kb), f, S[d]);
         }
         __syncthreads();
-        if (c + 1 < nc) {
-            stage_kt();
-            fetch_kt(next);
-        }
+        stage_kt();
+        fetch_kt(next);
     }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = gdn_row(d, 4 * g + r);
-            if (cv && row < a.dk) a.stateT[sbase + (size_t)row * a.dv] = S[d][r];
-        }
+    gdn_store_state(S, a.stateT + bh * sn, a.dk, a.dv, co);
 }
 
 template <int KTN, bool SAVE>

@@ -161,23 +161,18 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
     scan_wg_coords<true>(groups, grp, bh);
     const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
     const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
-    const int tid = threadIdx.x, w = tid >> 6, lane = lane_id(), r16 = lane & 15, g = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), r16 = lane & 15, g = lane >> 4;
     const int col = (grp * 4 + w) * 16 + r16;
     const bool cv = col < a.dv;
-    const size_t sbase = (size_t)bh * a.dk * a.dv + (cv ? col : 0);
+    const uint32_t co = cv ? col * 4 : GDN_OUT;
+    const size_t sn = (size_t)a.dk * a.dv;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
     sdm_f32x4 S[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = gdn_row(d, 4 * g + r);
-            S[d][r] = a.dstateT && cv && row < a.dk ? a.dstateT[sbase + (size_t)row * a.dv] : 0.f;
-        }
+    gdn_load_state(S, a.dstateT ? a.dstateT + bh * sn : nullptr, a.dk, a.dv, co);
     const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
-    const float* yp = a.dy + (size_t)bh * a.T * a.dv + (cv ? col : 0);
-    float* dvp = a.dvv + (size_t)bh * a.T * a.dv + col;
+    const float* yp = a.dy + (size_t)bh * a.T * a.dv;
+    float* dvp = a.dvv + (size_t)bh * a.T * a.dv;
     const size_t ch0 = (size_t)bh * a.nC, ck0 = (size_t)(b * a.Hk + hk) * a.nC;
 
     u4v rK[KTN], rT[9], rKT[KTN], rQT[KTN];
@@ -188,11 +183,11 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
     };
     const auto fetch_y = [&](int c) {
+        const auto buf = gdn_buf(yp + (size_t)c * GDN_C * a.dv, (size_t)min(len - c * GDN_C, GDN_C) * a.dv * 4);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                rY[m][r] = yp[(size_t)min(c * GDN_C + gdn_row(m, 4 * g + r), len - 1) * a.dv];
+            for (int r = 0; r < 4; ++r) rY[m][r] = gdn_ldf(buf, gdn_row(m, 4 * g + r) * a.dv * 4 + co);
     };
     const auto fetch_t = [&](int c) {
         const uint16_t* src = w < 2 ? a.tf : a.pf;
@@ -229,20 +224,14 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
     for (int c = nc - 1; c >= 0; --c) {
         const int t0 = c * GDN_C, left = len - t0, next = max(c - 2, 0);
         const float* vec = sV + (c & 1) * 3 * 64;
-        float* o = a.dS + (ch0 + c) * a.dk * a.dv + col;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = gdn_row(d, 4 * g + r);
-                if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
-            }
+        const auto rbuf = gdn_buf(dvp + (size_t)t0 * a.dv, (size_t)min(left, GDN_C) * a.dv * 4);
+        gdn_store_state(S, a.dS + (ch0 + c) * sn, a.dk, a.dv, co);
         sdm_f32x4 dE[4], Y[4], dR[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             dE[m] = dR[m] = zero;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) Y[m][r] = gdn_row(m, 4 * g + r) < left ? rY[m][r] : 0.f;
+            for (int r = 0; r < 4; ++r) Y[m][r] = rY[m][r];
         }
 #pragma unroll
         for (int kb = 0; kb < KTN; ++kb) {
@@ -254,14 +243,12 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
         for (int m = 0; m < 4; ++m) {
             const v4f en = ld4(vec + 64 + gdn_row(m, 4 * g));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dE[m][r] *= gdn_row(m, 4 * g + r) < left ? en[r] : 0.f;
+            for (int r = 0; r < 4; ++r) dE[m][r] *= en[r];
         }
         __syncthreads();
-        if (c > 0) {
-            stage_k((c - 1) & 1);
-            fetch_y(c - 1);
-            fetch_k(next);
-        }
+        stage_k((c + 1) & 1);
+        fetch_y(max(c - 1, 0));
+        fetch_k(next);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const GdnFrag<3> f = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
@@ -286,17 +273,15 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int t = gdn_row(m, 4 * g + r);
-                if (cv && t < left) dvp[(size_t)(t0 + t) * a.dv] = dR[m][r];
+                gdn_stf(rbuf, t * a.dv * 4 + co, dR[m][r]);
                 dR[m][r] *= -gam[r];
                 Y[m][r] *= gam[r];
             }
         }
         const float last = vec[63];
         __syncthreads();
-        if (c > 0) {
-            stage_t();
-            fetch_t(next);
-        }
+        stage_t();
+        fetch_t(next);
 #pragma unroll
         for (int d = 0; d < DT; ++d) S[d] *= last;
 #pragma unroll
@@ -310,20 +295,10 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
             }
         }
         __syncthreads();
-        if (c > 0) {
-            stage_kt();
-            fetch_kt(next);
-        }
+        stage_kt();
+        fetch_kt(next);
     }
-    if (a.dstate0) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = gdn_row(d, 4 * g + r);
-                if (cv && row < a.dk) a.dstate0[sbase + (size_t)row * a.dv] = S[d][r];
-            }
-    }
+    if (a.dstate0) gdn_store_state(S, a.dstate0 + bh * sn, a.dk, a.dv, co);
 }
 
 template <int KTN>
