@@ -454,6 +454,48 @@ int sdm_gdn_bwd(const void* q, const void* k, const void* v, int in_dtype, const
 size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v, int in_dtype);
 
 /* ------------------------------------------------------------------------
+ * sdm_linear — the projections on either side of a layer (Sec. 3.1: W_q, W_k, W_v,
+ * W_a, W_b, W_g before the recurrence; W_o and the residual stream after it):
+ *   z = x W^T + bias;  y = act(z) + residual
+ *   x         [B, T, K], or head-major [B, x_heads, T, K / x_heads] where
+ *             x_heads > 0 (feature h (K / x_heads) + c is head h's value c), in x_dtype.
+ *   w         [N, K] in w_dtype.  Types: both fp32, both bf16, or an fp32 x
+ *             with a bf16 w: x is then rounded to bf16 as it is read (the
+ *             epilogue's rows, which sdm_norm_gate leaves in fp32).
+ *   bias      [N] fp32 or NULL;  act  0 identity, 1 SiLU, 2 GELU (erf form).
+ *   residual  [B, T, N] in y_dtype or NULL; only with y_heads = 0.
+ *   y         out [B, T, N], or head-major [B, y_heads, T, N / y_heads] as the
+ *             recurrences read it, in y_dtype: w's type, or fp32.
+ *   z         optional out, laid out and typed as y, for sdm_linear_bwd.
+ * Sums are fp32; bf16 products are exact, fp32 ones fp32.  Sums over split
+ * depths are added in a fixed order: results are the same from run to run.
+ * y may be residual; no other output may overlap an input.
+ *   workspace  at least sdm_linear_workspace_bytes() bytes, 256-B aligned;
+ *              NULL where that is 0.
+ * Limits: K and K / x_heads multiples of 8 (bf16 w) or 4 (fp32); B T <= 2^30.
+ *
+ * sdm_linear_bwd — reverse mode, with dz = dy act'(z):
+ *   dx = dz W,  dw = dz^T x,  dbias[n] = sum over tokens of dz;  the gradient of
+ *   residual is dy itself.
+ *   dy        laid out as y, in dy_dtype: w's type, or fp32 (as the recurrences'
+ *             backwards write their gradients).  dz is rounded to w's type, in which
+ *             it enters the products; dbias sums it in fp32 before that.
+ *   z         as sdm_linear wrote it (z_dtype); NULL with act 0.
+ *   dx        optional out, laid out and typed as x;  dw  optional out [N, K] in
+ *             w_dtype;  dbias  optional out [N] fp32.
+ *   workspace  at least sdm_linear_bwd_workspace_bytes() bytes, 256-B aligned.
+ * ---------------------------------------------------------------------- */
+int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const float* bias, int act,
+               const void* residual, int B, int T, int K, int N, int y_heads, void* y, int y_dtype, void* z,
+               void* workspace, size_t ws_bytes, void* stream);
+size_t sdm_linear_workspace_bytes(int x_dtype, int w_dtype, int B, int T, int K, int N);
+int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const void* z, int z_dtype,
+                   int act, const void* dy, int dy_dtype, int B, int T, int K, int N, int y_heads, void* dx, void* dw,
+                   float* dbias, void* workspace, size_t ws_bytes, void* stream);
+size_t sdm_linear_bwd_workspace_bytes(int x_dtype, int w_dtype, int act, int dy_dtype, int B, int T, int K, int N,
+                                      int y_heads);
+
+/* ------------------------------------------------------------------------
  * sdm_mem_init — initial memory per call.  The learned initial state M_0 of
  * Sec. 3.1 ("Learned Initial State") is one [H, N, d_v] parameter shared by
  * all sequences; every sequence starts from its own copy:
@@ -535,8 +577,8 @@ enum sdm_kernel {
     SDM_K_ADDRESS = 0, SDM_K_FWD_PREP = 1, SDM_K_FWD_SCAN = 2, SDM_K_BWD_PREP = 3,
     SDM_K_BWD_SCAN = 4, SDM_K_BWD_REDUCE = 5, SDM_K_ADDRESS_BWD = 6, SDM_K_MEM_INIT = 7,
     SDM_K_DECODE = 8, SDM_K_CHUNK_COEF = 9, SDM_K_CHUNK_SCAN = 10, SDM_K_NORM_GATE = 11, SDM_K_GATES = 12,
-    SDM_K_GDN_PREP = 13, SDM_K_GDN_SCAN = 14, SDM_K_GDN_STEP = 15, SDM_K_GDN_BWD = 16,
-    SDM_K_COUNT = 17
+    SDM_K_GDN_PREP = 13, SDM_K_GDN_SCAN = 14, SDM_K_GDN_STEP = 15, SDM_K_GDN_BWD = 16, SDM_K_LINEAR = 17,
+    SDM_K_COUNT = 18
 };
 int sdm_profile_enable(int on);
 /* Which kernel kinds the events bracket while profiling is enabled: bit k for

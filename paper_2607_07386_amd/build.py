@@ -18,7 +18,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libsdm.so")
 SOURCES = ["address.hip", "scan_prep.hip", "scan_fwd.hip", "scan_round.hip", "scan_bwd.hip", "scan_bwd_round.hip", "scan_chunk.hip", "gates.hip",
-           "noalloc.hip", "gdn.hip", "gdn_bwd.hip", "api.cpp", "gdn_api.cpp"]
+           "noalloc.hip", "gdn.hip", "gdn_bwd.hip", "linear.hip", "api.cpp", "gdn_api.cpp",
+           "linear_api.cpp"]
 ARCH = os.environ.get("SDM_OFFLOAD_ARCH", "gfx950")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,50 @@
+// Projections: launch arguments shared by the kernels and the C ABI.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+// A matrix of `rows` x `cols` values in memory, flat [B, T, cols] or head-major
+// [B, heads, T, cols / heads]:
+//   offset(i, j) = (i / T) sb + (i % T) st + (j / d) sh + j % d.
+struct LinMat {
+    const void* p;
+    int dtype;
+    int rows, cols;
+    int T, d;
+    int64_t sb, st, sh;
+};
+inline LinMat lin_flat(const void* p, int dtype, int rows, int cols, int64_t ld) {
+    return {p, dtype, rows, cols, rows > 0 ? rows : 1, cols > 0 ? cols : 1, 0, ld, 0};
+}
+inline LinMat lin_tokens(const void* p, int dtype, int B, int T, int cols, int heads) {
+    if (heads <= 0) return lin_flat(p, dtype, B * T, cols, cols);
+    const int d = cols / heads, t = T > 0 ? T : 1;
+    return {p, dtype, B * T, cols, t, d, (int64_t)t * cols, d, (int64_t)t * d};
+}
+
+// C[i, j] = sum_r A(i, r) B(j, r).  ta: A is stored with r as its row index and i as
+// its column index (tb likewise); otherwise the other way round.
+struct LinGemm {
+    LinMat a, b;
+    bool ta, tb;
+    int I, J, R;          // output rows, output columns, depth
+    int ctype;            // type the factors enter the matrix cores in
+    // out = act(C + bias) + residual, pre = C + bias; both laid out as `out`
+    LinMat out;
+    void* pre;
+    const float* bias;
+    const void* residual;
+    int act;
+    // depth split over `split` workgroups: fp32 partial sums [split][I][J], added up by a second launch
+    int split;
+    float* part;
+};
+
+int sdm_linear_split(int I, int J, int R, int ctype);
+hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st);
+// dz = dy act'(z) as rows [M][ldz] of ctype (zeros past N), and dbias = column sums of it
+// (through parts [nparts][N] added in order).
+int sdm_linear_dz_parts(int M);
+hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int ctype, int ldz, void* dz,
+                                float* part, float* dbias, hipStream_t st);
+hipError_t sdm_launch_linear_zero(void* p, size_t words, hipStream_t st);

@@ -1,0 +1,270 @@
+// Projections (gfx950): y = act(x W^T + bias) + residual and its gradients, the
+// products on either side of the layer's recurrence (Sec. 3.1: W_q, W_k, W_v, W_a,
+// W_b, W_g before it, W_o and the residual stream after it), reading and writing the
+// recurrences' head-major layout.
+//   forward   C[m, n] = sum_k x[m, k] w[n, k]
+//   dx        C[m, k] = sum_n dz[m, n] w[n, k],   dz = dy act'(z)
+//   dw        C[n, k] = sum_m dz[m, n] x[m, k],   dbias[n] = sum_m dz[m, n]
+#include <algorithm>
+
+#include "linear.h"
+#include "sdm_common.h"
+#include "sdm_internal.h"
+
+namespace {
+
+__device__ __forceinline__ int64_t mat_off(const LinMat& m, int i, int j) {
+    return (int64_t)(i / m.T) * m.sb + (int64_t)(i % m.T) * m.st + (int64_t)(j / m.d) * m.sh + j % m.d;
+}
+__device__ __forceinline__ int64_t mat_row(const LinMat& m, int i) {
+    return (int64_t)(i / m.T) * m.sb + (int64_t)(i % m.T) * m.st;
+}
+__device__ __forceinline__ int64_t mat_col(const LinMat& m, int j) { return (int64_t)(j / m.d) * m.sh + j % m.d; }
+
+// round to nearest even
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ __forceinline__ void put(bf16_t* p, float x) { p->bits = bf16_bits(x); }
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+
+constexpr float kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
+__device__ __forceinline__ float lin_act(float z, int act) {
+    if (act == 1) return z * sdm_sigmoid(z);
+    if (act == 2) return 0.5f * z * (1.f + erff(z * kSqrtHalf));
+    return z;
+}
+__device__ __forceinline__ float lin_act_slope(float z, int act) {
+    if (act == 1) {
+        const float s = sdm_sigmoid(z);
+        return s * (1.f + z * (1.f - s));
+    }
+    if (act == 2) return 0.5f * (1.f + erff(z * kSqrtHalf)) + z * expf(-0.5f * z * z) * kInvSqrt2Pi;
+    return 1.f;
+}
+
+__device__ __forceinline__ float ld_any(const void* p, int dtype, int64_t i) {
+    return dtype == SDM_DT_F32 ? static_cast<const float*>(p)[i] : to_f32(static_cast<const bf16_t*>(p)[i]);
+}
+__device__ __forceinline__ void st_any(void* p, int dtype, int64_t i, float x) {
+    if (dtype == SDM_DT_F32) static_cast<float*>(p)[i] = x;
+    else put(static_cast<bf16_t*>(p) + i, x);
+}
+
+// one value of the result through the epilogue
+__device__ __forceinline__ void lin_store(const LinGemm& g, int i, int j, float c) {
+    if (g.bias) c += g.bias[j];
+    const int64_t o = mat_off(g.out, i, j);
+    if (g.pre) st_any(g.pre, g.out.dtype, o, c);
+    c = lin_act(c, g.act);
+    if (g.residual) c += ld_any(g.residual, g.out.dtype, o);
+    st_any(const_cast<void*>(g.out.p), g.out.dtype, o, c);
+}
+
+// ---------------------------------------------------------------- general kernel
+// 128 x 128 x 32 tiles for any sizes, layouts and types: LDS rows are output
+// indices, so a factor stored depth-first is turned while it is staged.
+constexpr int GT = 128, GK = 32;
+template <typename CT>
+struct GenTile;
+template <>
+struct GenTile<bf16_t> {
+    static constexpr int LD = GK + 8, PIECE = 8;
+};
+template <>
+struct GenTile<float> {
+    static constexpr int LD = GK + 4, PIECE = 4;
+};
+
+// PIECE consecutive values along the matrix's columns, as CT (zeros outside)
+template <typename CT, typename ST>
+__device__ __forceinline__ void gen_load(const LinMat& m, int row, int col, CT (&x)[GenTile<CT>::PIECE]) {
+    constexpr int P = GenTile<CT>::PIECE;
+    const bool ok = row < m.rows && col < m.cols;
+    const ST* p = static_cast<const ST*>(m.p) + (ok ? mat_off(m, row, col) : 0);
+#pragma unroll
+    for (int i = 0; i < P; i += 4) {
+        const v4f v = ok ? ld4v(p + i) : v4zero();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) put(&x[i + j], v[j]);
+    }
+}
+
+template <typename CT, typename ST, bool TR>
+__device__ __forceinline__ void gen_stage(const LinMat& m, int o0, int r0, CT* lds) {
+    constexpr int P = GenTile<CT>::PIECE, LD = GenTile<CT>::LD;
+    constexpr int per_row = (TR ? GT : GK) / P, rows = TR ? GK : GT;
+    for (int u = threadIdx.x; u < rows * per_row; u += 256) {
+        const int r = u / per_row, c = u % per_row * P;
+        CT x[P];
+        gen_load<CT, ST>(m, (TR ? r0 : o0) + r, (TR ? o0 : r0) + c, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            if constexpr (TR) lds[(c + i) * LD + r] = x[i];
+            else lds[r * LD + c + i] = x[i];
+        }
+    }
+}
+
+template <typename CT, typename AT, typename BT, bool TA, bool TB>
+__global__ __launch_bounds__(256) void linear_general_kernel(LinGemm g) {
+    constexpr int LD = GenTile<CT>::LD;
+    __shared__ __align__(16) CT sA[GT * LD], sB[GT * LD];
+    const int i0 = blockIdx.x * GT, j0 = blockIdx.y * GT;
+    const int lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+    const int wi = (w >> 1) * 64, wj = (w & 1) * 64;
+    sdm_f32x4 acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
+    const int steps = (g.R + GK - 1) / GK, per = (steps + g.split - 1) / g.split;
+    const int s0 = blockIdx.z * per, s1 = min(steps, s0 + per);
+    for (int s = s0; s < s1; ++s) {
+        gen_stage<CT, AT, TA>(g.a, i0, s * GK, sA);
+        gen_stage<CT, BT, TB>(g.b, j0, s * GK, sB);
+        __syncthreads();
+        if constexpr (sizeof(CT) == 2) {
+            sdm_bf16x8 fa[4], fb[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                fa[i] = *reinterpret_cast<const sdm_bf16x8*>(sA + (wi + 16 * i + r16) * LD + 8 * q);
+                fb[i] = *reinterpret_cast<const sdm_bf16x8*>(sB + (wj + 16 * i + r16) * LD + 8 * q);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int k = 0; k < GK; k += 4) {
+                float fa[4], fb[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    fa[i] = sA[(wi + 16 * i + r16) * LD + k + q];
+                    fb[i] = sB[(wj + 16 * i + r16) * LD + k + q];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int oi = i0 + wi + 16 * i + 4 * q + r, oj = j0 + wj + 16 * j + r16;
+                if (oi >= g.I || oj >= g.J) continue;
+                if (g.split > 1) g.part[((size_t)blockIdx.z * g.I + oi) * g.J + oj] = acc[i][j][r];
+                else lin_store(g, oi, oj, acc[i][j][r]);
+            }
+}
+
+// the partial sums of a split depth, added in order, through the epilogue
+__global__ __launch_bounds__(256) void linear_join_kernel(LinGemm g) {
+    const size_t n = (size_t)g.I * g.J;
+    for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < n; u += (size_t)gridDim.x * 256) {
+        float c = 0.f;
+        for (int s = 0; s < g.split; ++s) c += g.part[s * n + u];
+        lin_store(g, (int)(u / g.J), (int)(u % g.J), c);
+    }
+}
+
+// ---------------------------------------------------------------- dz, dbias
+// A workgroup takes 64 columns x `rows` rows: 16 columns-of-four lanes x 16 rows at a time.
+constexpr int DZ_ROWS = 256;
+template <typename CT>
+__global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z, int z_dtype, int act, int ldz,
+                                                        CT* dz, float* part) {
+    __shared__ float red[4][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), rg = threadIdx.x >> 6;
+    const int m0 = blockIdx.y * DZ_ROWS, m1 = min(dy.rows, m0 + DZ_ROWS);
+    float sum = 0.f;
+    if (c < ldz) {
+        const bool ok = c < dy.cols;
+        const int64_t co = ok ? mat_col(dy, c) : 0;
+        for (int m = m0 + rg; m < m1; m += 4) {
+            float v = 0.f;
+            if (ok) {
+                const int64_t o = mat_row(dy, m) + co;
+                v = ld_any(dy.p, dy.dtype, o);
+                if (act) v *= lin_act_slope(ld_any(z, z_dtype, o), act);
+                sum += v;
+            }
+            if (dz) put(dz + (size_t)m * ldz + c, v);
+        }
+    }
+    if (!part) return;
+    red[rg][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (rg == 0 && c < dy.cols)
+        part[(size_t)blockIdx.y * dy.cols + c] =
+            red[0][threadIdx.x] + red[1][threadIdx.x] + red[2][threadIdx.x] + red[3][threadIdx.x];
+}
+__global__ __launch_bounds__(256) void linear_colsum_kernel(const float* part, int parts, int N, float* out) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= N) return;
+    float s = 0.f;
+    for (int p = 0; p < parts; ++p) s += part[(size_t)p * N + c];
+    out[c] = s;
+}
+
+__global__ __launch_bounds__(256) void linear_zero_kernel(uint32_t* p, size_t n) {
+    for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < n; u += (size_t)gridDim.x * 256) p[u] = 0u;
+}
+
+template <typename CT, typename AT, typename BT>
+hipError_t launch_general(const LinGemm& g, hipStream_t st) {
+    const dim3 grid((g.I + GT - 1) / GT, (g.J + GT - 1) / GT, g.split);
+    if (!g.ta && !g.tb) linear_general_kernel<CT, AT, BT, false, false><<<grid, 256, 0, st>>>(g);
+    else if (!g.ta) linear_general_kernel<CT, AT, BT, false, true><<<grid, 256, 0, st>>>(g);
+    else linear_general_kernel<CT, AT, BT, true, true><<<grid, 256, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// Workgroups that share a tile's depth: as many as fill the device, each with
+// 256 depths or more.
+int sdm_linear_split(int I, int J, int R, int ctype) {
+    const int64_t tiles = (int64_t)((I + GT - 1) / GT) * ((J + GT - 1) / GT);
+    const int cus = sdm_device_simds() / 4;
+    const int64_t want = (2 * cus + tiles - 1) / std::max<int64_t>(tiles, 1), most = std::max(R / 256, 1);
+    return tiles * 2 > cus ? 1 : (int)std::max<int64_t>(1, std::min(want, most));
+}
+
+hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st) {
+    hipError_t e;
+    if (g.ctype == SDM_DT_F32) e = launch_general<float, float, float>(g, st);
+    else if (g.a.dtype == SDM_DT_F32) e = launch_general<bf16_t, float, bf16_t>(g, st);
+    else if (g.b.dtype == SDM_DT_F32) e = launch_general<bf16_t, bf16_t, float>(g, st);
+    else e = launch_general<bf16_t, bf16_t, bf16_t>(g, st);
+    if (e != hipSuccess || g.split <= 1) return e;
+    const size_t n = (size_t)g.I * g.J;
+    linear_join_kernel<<<(int)std::min<size_t>((n + 255) / 256, 8192), 256, 0, st>>>(g);
+    return hipGetLastError();
+}
+
+int sdm_linear_dz_parts(int M) { return (M + DZ_ROWS - 1) / DZ_ROWS; }
+
+hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int ctype, int ldz, void* dz,
+                                float* part, float* dbias, hipStream_t st) {
+    const int parts = sdm_linear_dz_parts(dy.rows);
+    const dim3 grid((ldz + 63) / 64, parts);
+    float* p = dbias ? part : nullptr;
+    if (ctype == SDM_DT_F32)
+        linear_dz_kernel<float><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, ldz, static_cast<float*>(dz), p);
+    else linear_dz_kernel<bf16_t><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, ldz, static_cast<bf16_t*>(dz), p);
+    if (dbias) linear_colsum_kernel<<<(dy.cols + 255) / 256, 256, 0, st>>>(part, parts, dy.cols, dbias);
+    return hipGetLastError();
+}
+
+hipError_t sdm_launch_linear_zero(void* p, size_t words, hipStream_t st) {
+    linear_zero_kernel<<<(int)std::min<size_t>((words + 255) / 256, 8192), 256, 0, st>>>(static_cast<uint32_t*>(p), words);
+    return hipGetLastError();
+}

@@ -82,6 +82,12 @@ def lib() -> ctypes.CDLL:
         L.sdm_gdn_saved_bytes.argtypes = [I, I, I, I, I]
         for f in ("sdm_gdn_fwd_workspace_bytes", "sdm_gdn_bwd_workspace_bytes", "sdm_gdn_saved_bytes"):
             getattr(L, f).restype = SZ
+        L.sdm_linear.argtypes = [P, I, I, P, I, P, I, P, I, I, I, I, I, P, I, P, P, SZ, P]
+        L.sdm_linear_bwd.argtypes = [P, I, I, P, I, P, I, I, P, I, I, I, I, I, I, P, P, P, P, SZ, P]
+        L.sdm_linear_workspace_bytes.argtypes = [I, I, I, I, I, I]
+        L.sdm_linear_bwd_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I, I]
+        L.sdm_linear_workspace_bytes.restype = SZ
+        L.sdm_linear_bwd_workspace_bytes.restype = SZ
         L.sdm_check_device_errors.argtypes = [P, P]
         L.sdm_profile_enable.argtypes = [I]
         L.sdm_profile_select.argtypes = [ctypes.c_uint]
@@ -97,6 +103,7 @@ def lib() -> ctypes.CDLL:
         for f in ("sdm_address", "sdm_scan_fwd", "sdm_scan_fwd_chunked", "sdm_scan_bwd", "sdm_mem_init",
                   "sdm_forward_noalloc", "sdm_gates", "sdm_gates_bwd", "sdm_norm_gate", "sdm_norm_gate_bwd",
                   "sdm_layer_fwd", "sdm_layer_bwd", "sdm_gdn_fwd", "sdm_gdn_bwd",
+                  "sdm_linear", "sdm_linear_bwd",
                   "sdm_check_device_errors",
                   "sdm_profile_enable", "sdm_profile_select", "sdm_profile_read"):
             getattr(L, f).restype = I
@@ -706,6 +713,104 @@ def gdn_bwd(q, k, v, alpha, beta, saved, dy, dstate_T=None, lens=None, workspace
     return out
 
 
+def _tokens_of(x, name):
+    """(B, T, features, heads) of [B,T,features] (heads 0) or head-major [B,heads,T,d]."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.dim() == 3:
+        return x.shape[0], x.shape[1], x.shape[2], 0
+    if x.dim() == 4:
+        return x.shape[0], x.shape[2], x.shape[1] * x.shape[3], x.shape[1]
+    raise ValueError(f"{name} must be [B,T,features] or [B,heads,T,d], got shape {tuple(x.shape)}")
+
+
+def _check_linear(x, w):
+    B, T, K, heads = _tokens_of(x, "x")
+    _expect_dims(w, "w", 2)
+    if w.dtype not in _IN:
+        raise TypeError(f"w has dtype {w.dtype}, expected float32 or bfloat16")
+    if x.dtype not in (w.dtype, torch.float32):
+        raise TypeError(f"x has dtype {x.dtype}, expected w's {w.dtype} or float32")
+    N = w.shape[0]
+    _expect(w, "w", (N, K), (w.dtype,))
+    return B, T, K, N, heads
+
+
+def linear_workspace(x, w) -> torch.Tensor:
+    B, T, K, N, _ = _check_linear(x, w)
+    return _ws(lib().sdm_linear_workspace_bytes(_dtype_code(x), _dtype_code(w), B, T, K, N), x.device)
+
+
+def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dtype=None, want_z: bool = False,
+           workspace=None, y=None):
+    """A projection: z = x w^T + bias, y = act(z) + residual (act 0 identity, 1 SiLU, 2 GELU).  x [B,T,K] or
+    head-major [B,heads,T,d] (K = heads d); w [N,K]; bias [N] fp32; residual [B,T,N] in y's dtype.  Returns y
+    [B,T,N], or head-major [B,heads,T,N/heads] where heads > 0, in out_dtype (w's by default, or float32), and
+    z (laid out and typed as y) if wanted.  An fp32 x with a bf16 w is rounded to bf16."""
+    B, T, K, N, x_heads = _check_linear(x, w)
+    heads = int(heads)
+    if heads < 0 or (heads and N % heads):
+        raise ValueError(f"heads {heads} must divide the {N} outputs")
+    if bias is not None:
+        _expect(bias, "bias", (N,), _F32)
+    dt = w.dtype if out_dtype is None else out_dtype
+    if dt not in (w.dtype, torch.float32):
+        raise TypeError(f"out_dtype must be w's {w.dtype} or float32, got {dt}")
+    if residual is not None:
+        if heads:
+            raise ValueError("a residual needs a flat output (heads 0)")
+        _expect(residual, "residual", (B, T, N), (dt,))
+    shape = (B, heads, T, N // heads) if heads else (B, T, N)
+    if y is not None:
+        _expect(y, "y", shape, (dt,))
+    need = lib().sdm_linear_workspace_bytes(_dtype_code(x), _dtype_code(w), B, T, K, N)
+    _check_ws(workspace, need)
+    dev = _dev(x, w, bias, residual, workspace, y)
+    if y is None:
+        y = torch.empty(shape, dtype=dt, device=dev)
+    z = torch.empty_like(y) if want_z else None
+    if workspace is None and need:
+        workspace = _ws(need, dev)
+    with _current(dev):
+        rc = lib().sdm_linear(_ptr(x), _dtype_code(x), x_heads, _ptr(w), _dtype_code(w), _ptr(bias), int(act),
+                              _ptr(residual), B, T, K, N, heads, _ptr(y), _dtype_code(y), _ptr(z), _ptr(workspace),
+                              0 if workspace is None else workspace.numel(), _stream(dev))
+    _check("sdm_linear", rc)
+    return (y, z) if want_z else y
+
+
+def linear_bwd(x, w, dy, z=None, act: int = 0, want_dx: bool = True, want_dw: bool = True, want_dbias: bool = False,
+               workspace=None):
+    """Reverse mode of linear: dz = dy act'(z), dx = dz w, dw = dz^T x, dbias = sum dz (residual's gradient is
+    dy).  dy [B,T,N] or head-major [B,heads,T,N/heads], in w's dtype or float32; z as linear returned it (not
+    needed with act 0).  Returns a dict of dx (as x), dw (as w) and dbias (fp32); None where not wanted."""
+    B, T, K, N, x_heads = _check_linear(x, w)
+    dB, dT, dN, heads = _tokens_of(dy, "dy")
+    if (dB, dT, dN) != (B, T, N):
+        raise ValueError(f"dy has shape {tuple(dy.shape)}, expected {N} outputs for {B} x {T} tokens")
+    if dy.dtype not in (w.dtype, torch.float32):
+        raise TypeError(f"dy has dtype {dy.dtype}, expected w's {w.dtype} or float32")
+    if act and z is None:
+        raise ValueError("z is required for an activation's gradient")
+    if z is not None:
+        _expect(z, "z", tuple(dy.shape), (w.dtype, torch.float32))
+    codes = _dtype_code(x), _dtype_code(w), _dtype_code(dy)
+    need = lib().sdm_linear_bwd_workspace_bytes(codes[0], codes[1], int(act), codes[2], B, T, K, N, heads)
+    _check_ws(workspace, need)
+    dev = _dev(x, w, dy, z, workspace)
+    out = dict(dx=torch.empty_like(x) if want_dx else None, dw=torch.empty_like(w) if want_dw else None,
+               dbias=torch.empty((N,), dtype=torch.float32, device=dev) if want_dbias else None)
+    if workspace is None:
+        workspace = _ws(need, dev)
+    with _current(dev):
+        rc = lib().sdm_linear_bwd(_ptr(x), codes[0], x_heads, _ptr(w), codes[1], _ptr(z),
+                                  codes[1] if z is None else _dtype_code(z), int(act), _ptr(dy), codes[2], B, T, K, N,
+                                  heads, _ptr(out["dx"]), _ptr(out["dw"]), _ptr(out["dbias"]), _ptr(workspace),
+                                  workspace.numel(), _stream(dev))
+    _check("sdm_linear_bwd", rc)
+    return out
+
+
 def mem_init(dst: torch.Tensor, m0: torch.Tensor | None):
     """dst [B,H,N,d_v] = m0 [H,N,d_v] broadcast over B (or zero when m0 is None)."""
     _expect_dims(dst, "dst", 4)
@@ -726,7 +831,7 @@ def check_device_errors(workspace: torch.Tensor):
 
 KERNELS = {"address": 0, "fwd_prep": 1, "fwd_scan": 2, "bwd_prep": 3, "bwd_scan": 4, "bwd_reduce": 5,
            "address_bwd": 6, "mem_init": 7, "decode": 8, "chunk_coef": 9, "chunk_scan": 10, "norm_gate": 11,
-           "gates": 12, "gdn_prep": 13, "gdn_scan": 14, "gdn_step": 15, "gdn_bwd": 16}
+           "gates": 12, "gdn_prep": 13, "gdn_scan": 14, "gdn_step": 15, "gdn_bwd": 16, "linear": 17}
 
 
 def set_chunk_scan_cols(cols: int):

@@ -1,0 +1,225 @@
+"""The projections against fp64, forward and backward, flat and head-major.
+
+Tolerance, relative to the largest value.  fp32: a sum of n terms is off by at most
+n roundings of 2^-24 of the terms' magnitudes together, whose sum is at most about
+sqrt(n) times the result's largest value for terms of either sign: sqrt(n) n 2^-24 in
+the worst case, n 2^-24 where roundings fall either way (4e-5 at n = 700); activations add
+a few roundings.  bf16: inputs are exact, sums as before, and one rounding of the result,
+2^-8 at most; gradients enter through dz rounded to bf16 as well, at most 2^-8 of each
+term, so of the sum of magnitudes: 2^-8 sqrt(n) in the worst case, and 2^-8 where they
+fall either way.  Twice 2^-8 covers both roundings.  An fp32 x rounded to bf16 counts
+like dz."""
+import pytest
+import torch
+
+from paper_2607_07386_amd import sdm
+from tests.gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+F32_TOL, BF16_TOL = 4e-5, 2 * 2.0 ** -8
+ACTS = [lambda z: z, torch.nn.functional.silu, torch.nn.functional.gelu]
+
+
+def close(got, ref, what, tol):
+    ref = ref.detach()
+    assert got.shape == ref.shape, what
+    if ref.numel():
+        e = ((got.double() - ref).abs().max() / ref.abs().max().clamp_min(1e-30)).item()
+        assert e <= tol, f"{what}: {e:.2e}"
+
+
+def flat(x):
+    return x.transpose(1, 2).flatten(-2) if x.dim() == 4 else x
+
+
+def case(B, T, K, N, hin, hout, bf16, x_f32=False, seed=0):
+    g = torch.Generator(device=DEV).manual_seed(seed + B * T + K + N)
+    n = lambda *s: torch.randn(s, generator=g, device=DEV)
+    dt = torch.bfloat16 if bf16 else torch.float32
+    x = n(B, hin, T, K // hin) if hin else n(B, T, K)
+    return (x if x_f32 else x.to(dt), (n(N, K) / K ** 0.5).to(dt), n(N), n(B, T, N).to(dt),
+            (n(B, hout, T, N // hout) if hout else n(B, T, N)).to(dt))
+
+
+def reference(x, w, bias, act, residual, hout):
+    z = flat(x) @ w.T
+    z = z if bias is None else z + bias
+    y = ACTS[act](z)
+    y = y if residual is None else y + residual
+    to = lambda a: a.unflatten(-1, (hout, -1)).transpose(1, 2) if hout else a
+    return to(y), to(z)
+
+
+SHAPES = [  # B, T, K, N, heads in, heads out
+    (1, 1, 8, 1, 0, 0), (3, 1, 64, 7, 0, 7), (16, 1, 256, 512, 0, 4), (2, 33, 40, 130, 5, 0), (1, 129, 136, 65, 0, 5),
+    (2, 257, 96, 96, 2, 3), (1, 300, 704, 260, 0, 0), (3, 50, 520, 24, 13, 12), (1, 640, 512, 512, 8, 8),
+    (5, 1, 1024, 1, 0, 0), (2, 512, 256, 384, 2, 6), (1, 1, 4096, 300, 0, 0),
+]
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mixed", "bf16_to_f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_forward(shape, kind, act):
+    B, T, K, N, hin, hout = shape
+    bf = kind != "f32"
+    x, w, bias, res, _ = case(B, T, K, N, hin, hout, bf, kind == "mixed")
+    out = torch.float32 if kind == "bf16_to_f32" else None
+    tol = F32_TOL if kind in ("f32", "bf16_to_f32") else BF16_TOL
+    for b in (None, bias):
+        for r in (None, res) if not hout else (None,):
+            r = r if r is None or out is None else r.float()
+            y, z = sdm.linear(x, w, b, act=act, residual=r, heads=hout, out_dtype=out, want_z=True)
+            ry, rz = reference(x.double(), w.double(), None if b is None else b.double(), act,
+                               None if r is None else r.double(), hout)
+            assert y.dtype == (out or w.dtype)
+            close(y, ry, "y", tol)
+            close(z, rz, "z", tol)
+    assert torch.equal(y, sdm.linear(x, w, b, act=act, residual=r, heads=hout, out_dtype=out))
+
+
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mixed", "bf16_dy_f32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_gradients(shape, kind, act):
+    B, T, K, N, hin, hout = shape
+    bf = kind != "f32"
+    x, w, bias, _, dy = case(B, T, K, N, hin, hout, bf, kind == "mixed")
+    if kind == "bf16_dy_f32":
+        dy = dy.float() * 1.001
+    y, z = sdm.linear(x, w, bias, act=act, heads=hout, want_z=True)
+    g = sdm.linear_bwd(x, w, dy, z=z if act else None, act=act, want_dbias=True)
+    # the derivative at the z that was kept (its rounding is the forward's, not the gradients')
+    zd = flat(z.double()).requires_grad_()
+    dz, = torch.autograd.grad(ACTS[act](zd), zd, flat(dy.double()))
+    dz = dz.flatten(0, 1)
+    xd = flat(x.double()).flatten(0, 1)
+    dx = (dz @ w.double()).view(B, T, K)
+    dx = dx.unflatten(-1, (hin, -1)).transpose(1, 2) if hin else dx
+    tol = BF16_TOL if bf else F32_TOL
+    assert g["dx"].dtype == x.dtype and g["dw"].dtype == w.dtype
+    close(g["dx"], dx, "dx", tol)
+    close(g["dw"], dz.T @ xd, "dw", tol)
+    close(g["dbias"], dz.sum(0), "dbias", F32_TOL)
+    g2 = sdm.linear_bwd(x, w, dy, z=z, act=act, want_dx=False)
+    assert g2["dx"] is None and g2["dbias"] is None and torch.equal(g2["dw"], g["dw"])
+    g3 = sdm.linear_bwd(x, w, dy, z=z, act=act, want_dw=False)
+    assert torch.equal(g3["dx"], g["dx"])
+
+
+def test_gradients_against_differences():
+    x, w, bias, _, dy = case(2, 20, 16, 12, 0, 3, False)
+    for act in (1, 2):
+        _, z = sdm.linear(x, w, bias, act=act, heads=3, want_z=True)
+        g = sdm.linear_bwd(x, w, dy, z=z, act=act, want_dbias=True)
+        at = dict(x=x.double(), w=w.double(), bias=bias.double())
+        loss = lambda a: (reference(a["x"], a["w"], a["bias"], act, None, 3)[0] * dy).sum()
+        for name in at:
+            way = torch.randn_like(at[name])
+            d = (loss({**at, name: at[name] + 1e-5 * way}) - loss({**at, name: at[name] - 1e-5 * way})) / 2e-5
+            got = g["d" + name].double() * way
+            assert abs(got.sum() - d) <= F32_TOL * got.abs().sum(), name
+
+
+def test_no_tokens():
+    w, b = torch.randn(24, 16, device=DEV), torch.randn(24, device=DEV)
+    x = torch.empty((2, 0, 16), device=DEV)
+    assert sdm.linear(x, w, b).shape == (2, 0, 24)
+    g = sdm.linear_bwd(x, w, torch.empty((2, 0, 24), device=DEV), want_dbias=True)
+    assert g["dx"].shape == x.shape and not g["dw"].any() and not g["dbias"].any()
+
+
+def test_infinities_stay_in_their_rows():
+    """A row's infinity or NaN touches no other row (and no padding of a tile gets in)."""
+    x, w, bias, _, _ = case(1, 70, 64, 40, 0, 0, True)
+    y0 = sdm.linear(x, w, bias)
+    x[0, 5, 3], x[0, 69, 0] = float("inf"), float("nan")
+    y = sdm.linear(x, w, bias)
+    keep = [i for i in range(70) if i not in (5, 69)]
+    assert torch.equal(y[:, keep], y0[:, keep])
+    assert not torch.isfinite(y[0, 5]).any() and torch.isnan(y[0, 69]).all()
+
+
+def test_in_place_residual_stream_and_graph():
+    B, T, K, N = 2, 100, 128, 96
+    x, w, bias, res, dy = case(B, T, K, N, 0, 0, True)
+    y = sdm.linear(x, w, bias, act=1, residual=res)
+    mine = res.clone()
+    sdm.linear(x, w, bias, act=1, residual=mine, y=mine)
+    assert torch.equal(mine, y)
+    xs = x.clone()
+
+    def step():
+        y, z = sdm.linear(xs, w, bias, act=1, residual=res, want_z=True)
+        return dict(y=y, **sdm.linear_bwd(xs, w, dy, z=z, act=1, want_dbias=True))
+
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g = step()
+    for turn in range(3):
+        xs.copy_(x * (turn + 1))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {a: t.clone() for a, t in g.items()}
+        for a, t in step().items():
+            assert torch.equal(t, got[a]), a
+
+
+def test_layer_from_stream_to_stream():
+    """x -> projections (head-major) -> gates -> dense rule -> gated norm -> output projection + residual,
+    and back, as a layer chains them; fp32, against the derivative in 64 bits."""
+    B, T, D, H, d = 2, 100, 48, 3, 16
+    g = torch.Generator(device=DEV).manual_seed(0)
+    n = lambda *s: torch.randn(s, generator=g, device=DEV)
+    x, dout = n(B, T, D), n(B, T, D)
+    wq, wk, wv, wg = (n(H * d, D) / D ** 0.5 / 2 for _ in range(4))
+    wa, wb, wo = n(H, D) / D ** 0.5, n(H, D) / D ** 0.5, n(D, H * d) / (H * d) ** 0.5
+    A, b_dt, gamma = n(H).abs(), n(H), n(d)
+    q, k, v, gate = (sdm.linear(x, w, heads=H) for w in (wq, wk, wv, wg))
+    k = k * 0.25      # so that beta |k|^2 stays small and the update contracts
+    a_pre, b_pre = (sdm.linear(x, w, heads=H)[..., 0].contiguous() for w in (wa, wb))
+    al, be = sdm.gates(a_pre, b_pre, A, b_dt)
+    saved = sdm.gdn_saved_buffer(B, H, T, d, d, torch.device(DEV))
+    y, _ = sdm.gdn_fwd(q, k, v, al, be, saved=saved)
+    o = sdm.norm_gate(y, gate, gamma, 1e-5, 1)
+    out = sdm.linear(o, wo, residual=x)
+    go = sdm.linear_bwd(o, wo, dout)
+    dy, dgate, _ = sdm.norm_gate_bwd(y, gate, gamma, 1e-5, 1, go["dx"])
+    gr = sdm.gdn_bwd(q, k, v, al, be, saved, dy)
+    da, db, _, _ = sdm.gates_bwd(a_pre, b_pre, A, b_dt, gr["dalpha"], gr["dbeta"])
+    dx, dws = dout.clone(), {}
+    for name, w, grad in (("q", wq, gr["dq"]), ("k", wk, gr["dk"] * 0.25), ("v", wv, gr["dv"]), ("g", wg, dgate),
+                          ("a", wa, da[..., None].contiguous()), ("b", wb, db[..., None].contiguous())):
+        s = sdm.linear_bwd(x, w, grad)
+        dx += s["dx"]
+        dws[name] = s["dw"]
+    leaves = [t.double().requires_grad_() for t in (x, wq, wk, wv, wg, wa, wb, wo)]
+    X, WQ, WK, WV, WG, WA, WB, WO = leaves
+    F = torch.nn.functional
+    split = lambda z: z.unflatten(-1, (H, -1)).transpose(1, 2)
+    Q, K_, V, Gt = split(X @ WQ.T), split(X @ WK.T) * 0.25, split(X @ WV.T), split(X @ WG.T)
+    al_ = torch.exp(-A.double()[:, None] * F.softplus((X @ WA.T).transpose(1, 2) + b_dt.double()[:, None]))
+    be_ = (X @ WB.T).transpose(1, 2).sigmoid()
+    S, ys = torch.zeros((B, H, d, d), dtype=torch.float64, device=DEV), []
+    for t in range(T):
+        kt = K_[:, :, t, :, None]
+        Dm = al_[:, :, t, None, None] * S
+        S = Dm + kt * (be_[:, :, t, None] * (V[:, :, t] - (kt * Dm).sum(-2)))[:, :, None]
+        ys.append((Q[:, :, t, :, None] * S).sum(-2))
+    Y = torch.stack(ys, 2)
+    O = Y * torch.rsqrt(Y.square().mean(-1, keepdim=True) + 1e-5) * gamma.double() * F.silu(Gt)
+    ref = O.transpose(1, 2).flatten(-2) @ WO.T + X
+    grads = torch.autograd.grad(ref, leaves, dout.double())
+    # five operators one after the other, each within F32_TOL of its own inputs
+    tol = 5 * F32_TOL
+    close(out, ref, "out", tol)
+    close(dx, grads[0], "dx", tol)
+    for name, r in zip("qkvgab", grads[1:7]):
+        close(dws[name], r, "dw" + name, tol)
+    close(go["dw"], grads[7], "dwo", tol)
