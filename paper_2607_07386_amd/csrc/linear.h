@@ -37,10 +37,15 @@ struct LinGemm {
     int act;
     // depth split over `split` workgroups: fp32 partial sums [split][I][J], added up by a second launch
     int split;
+    bool big;
     float* part;
 };
 
-int sdm_linear_split(int I, int J, int R, int ctype);
+struct LinPlan {
+    bool big;
+    int split;
+};
+LinPlan sdm_linear_plan(int I, int J, int R, int ctype);
 hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st);
 // dz = dy act'(z) as rows [M][ldz] of ctype (zeros past N), and dbias = column sums of it
 // (through parts [nparts][N] added in order).

@@ -175,6 +175,186 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinGemm g) {
     }
 }
 
+// ---------------------------------------------------------------- tiled kernel
+// bf16 factors: BM x BN x 64 tiles, WR x WC waves of 32x32x16 matrix instructions.
+// The next tile goes straight from memory to LDS while this one is multiplied; a
+// factor stored with its output index as the row is [BM][64] there, one stored depth
+// first stays [64][BM] and is turned by the transposing LDS reads.  A piece of 16
+// bytes stands at its place XOR a function of its row, so that the lanes of a
+// read fall on different banks (the pieces of one direct load go to consecutive
+// addresses, so the order is chosen by which piece a lane fetches).
+typedef float lin_f32x16 __attribute__((ext_vector_type(16)));
+typedef short lin_s4 __attribute__((ext_vector_type(4)));
+__device__ const uint4 lin_zeros = {0u, 0u, 0u, 0u};   // what pieces outside a matrix read
+
+constexpr int BK = 64;
+
+__device__ __forceinline__ void dma16(const void* g, void* l) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
+                                     (__attribute__((address_space(3))) void*)l, 16, 0, 0);
+}
+
+// A factor's tile: O output indices x 64 depths.  Each of the NW waves moves O / (8 NW)
+// runs of 1 KB.
+template <int O, int NW, bool TR>
+struct LinTile {
+    static constexpr int RUNS = O / (8 * NW);
+    static constexpr int PPR = (TR ? O : BK) / 8;      // pieces of a row of the tile in LDS
+    static constexpr int RPR = 64 / PPR;               // rows of a run
+    static constexpr int MASK = PPR / 4 - 1;           // TR: 4 pieces (32 outputs) move together
+    const bf16_t* p[RUNS];   // !TR: the lane's rows (NULL past the end)
+    int run0, row, piece;    // lane's place in a run
+
+    __device__ __forceinline__ static int swz(int r) { return TR ? 4 * (r & MASK) : r & 7; }
+
+    __device__ __forceinline__ void init(const LinMat& m, int o0) {
+        const int lane = lane_id(), w = threadIdx.x >> 6;
+        run0 = w * RUNS;
+        row = lane / PPR;
+        piece = lane % PPR;
+        if constexpr (!TR) {
+            piece ^= swz(row);   // rows of a run and of the next differ by 8: one piece for all
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i) {
+                const int o = o0 + (run0 + i) * RPR + row;
+                p[i] = o < m.rows ? static_cast<const bf16_t*>(m.p) + mat_row(m, o) : nullptr;
+            }
+        }
+    }
+    __device__ __forceinline__ void fetch(const LinMat& m, int o0, int r0, unsigned char* lds) {
+        const bool heads = m.T != m.rows || m.d != m.cols;
+        if constexpr (!TR) {
+            const int c = r0 + piece * 8;
+            const int64_t off = heads ? mat_col(m, c) : c;
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i) {
+                const void* g = p[i] && c < m.cols ? (const void*)(p[i] + off) : (const void*)&lin_zeros;
+                dma16(g, lds + (run0 + i) * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i) {
+                const int kr = (run0 + i) * RPR + row, r = r0 + kr;
+                const int c = o0 + ((piece ^ swz(kr)) * 8);
+                const void* g = &lin_zeros;
+                if (r < m.rows && c < m.cols)
+                    g = static_cast<const bf16_t*>(m.p) + (heads ? mat_off(m, r, c) : (int64_t)r * m.st + c);
+                dma16(g, lds + (run0 + i) * 1024);
+            }
+        }
+    }
+    // 32 outputs from `o` on, depths 16 kk .. 16 kk + 15: output = lane & 31, 8 depths a lane half
+    __device__ __forceinline__ static sdm_bf16x8 frag(const unsigned char* lds, int o, int kk) {
+        const int lane = lane_id();
+        if constexpr (!TR) {
+            const int r = o + (lane & 31), c = (2 * kk + (lane >> 5)) ^ swz(r);
+            return *reinterpret_cast<const sdm_bf16x8*>(lds + r * 128 + c * 16);
+        } else {
+            const int k = 16 * kk + 8 * (lane >> 5) + ((lane & 15) >> 2);
+            const int c = o / 8 + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+            union {
+                lin_s4 s[2];
+                sdm_bf16x8 v;
+            } f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char* a = lds + (k + 4 * h) * (O * 2) + (c ^ swz(k + 4 * h)) * 16 + (lane & 1) * 8;
+                f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) lin_s4*)a);
+            }
+            return f.v;
+        }
+    }
+};
+
+template <int BM, int BN, int WR, int WC, bool TA, bool TB>
+__global__ __launch_bounds__(WR* WC * 64) void linear_tile_kernel(LinGemm g, int tiles_j) {
+    constexpr int NW = WR * WC, MI = BM / WR / 32, NJ = BN / WC / 32;
+    __shared__ __align__(1024) unsigned char sA0[BM * BK * 2], sA1[BM * BK * 2], sB0[BN * BK * 2], sB1[BN * BK * 2];
+    using TileA = LinTile<BM, NW, TA>;
+    using TileB = LinTile<BN, NW, TB>;
+
+    // Workgroups go to the 8 XCDs in turn: give each a contiguous range of tiles, and walk
+    // the range in columns of 8 row tiles, so that an L2 sees few rows and columns at a time.
+    const int tiles_i = (g.I + BM - 1) / BM, n = tiles_i * tiles_j;
+    int id = blockIdx.x;
+    {
+        const int q = n / 8, rem = n % 8, x = id % 8;
+        id = (x < rem ? x * (q + 1) : rem * (q + 1) + (x - rem) * q) + id / 8;
+    }
+    const int band = id / (8 * tiles_j), in = id % (8 * tiles_j), bh = min(8, tiles_i - 8 * band);
+    const int i0 = (8 * band + in % bh) * BM, j0 = in / bh * BN;
+
+    const int lane = lane_id(), w = threadIdx.x >> 6;
+    const int wi = w / WC * (BM / WR), wj = w % WC * (BN / WC);
+    lin_f32x16 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+    const int steps = (g.R + BK - 1) / BK, per = (steps + g.split - 1) / g.split;
+    const int s0 = blockIdx.y * per, s1 = min(steps, s0 + per);
+    TileA ta;
+    TileB tb;
+    ta.init(g.a, i0);
+    tb.init(g.b, j0);
+    const auto fetch = [&](int s, unsigned char* la, unsigned char* lb) {
+        ta.fetch(g.a, i0, s * BK, la);
+        tb.fetch(g.b, j0, s * BK, lb);
+    };
+    const auto multiply = [&](const unsigned char* la, const unsigned char* lb) {
+#pragma unroll
+        for (int kk = 0; kk < BK / 16; ++kk) {
+            sdm_bf16x8 fa[MI], fb[NJ];
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[i] = TileA::frag(la, wi + 32 * i, kk);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) fb[j] = TileB::frag(lb, wj + 32 * j, kk);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        }
+    };
+    if (s0 < s1) fetch(s0, sA0, sB0);
+    for (int s = s0; s < s1; s += 2) {   // two buffers by name: the compiler sees which reads a load in flight concerns
+        __syncthreads();
+        if (s + 1 < s1) fetch(s + 1, sA1, sB1);
+        multiply(sA0, sB0);
+        if (s + 1 >= s1) break;
+        __syncthreads();
+        if (s + 2 < s1) fetch(s + 2, sA0, sB0);
+        multiply(sA1, sB1);
+    }
+    // C: column = lane & 31, rows 8 (e / 4) + 4 (lane >> 5) + e % 4
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const int oj = j0 + wj + 32 * j + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int oi = i0 + wi + 32 * i + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+                if (oi >= g.I || oj >= g.J) continue;
+                if (g.split > 1) g.part[((size_t)blockIdx.y * g.I + oi) * g.J + oj] = acc[i][j][e];
+                else lin_store(g, oi, oj, acc[i][j][e]);
+            }
+        }
+}
+
+template <int BM, int BN, int WR, int WC>
+hipError_t launch_tile(const LinGemm& g, hipStream_t st) {
+    const int ti = (g.I + BM - 1) / BM, tj = (g.J + BN - 1) / BN;
+    const dim3 grid(ti * tj, g.split);
+    if (!g.ta && !g.tb) linear_tile_kernel<BM, BN, WR, WC, false, false><<<grid, WR * WC * 64, 0, st>>>(g, tj);
+    else if (!g.ta) linear_tile_kernel<BM, BN, WR, WC, false, true><<<grid, WR * WC * 64, 0, st>>>(g, tj);
+    else linear_tile_kernel<BM, BN, WR, WC, true, true><<<grid, WR * WC * 64, 0, st>>>(g, tj);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- dz, dbias
 // A workgroup takes 64 columns x `rows` rows: 16 columns-of-four lanes x 16 rows at a time.
 constexpr int DZ_ROWS = 256;
@@ -229,13 +409,18 @@ hipError_t launch_general(const LinGemm& g, hipStream_t st) {
 
 }  // namespace
 
-// Workgroups that share a tile's depth: as many as fill the device, each with
-// 256 depths or more.
-int sdm_linear_split(int I, int J, int R, int ctype) {
-    const int64_t tiles = (int64_t)((I + GT - 1) / GT) * ((J + GT - 1) / GT);
+// Tile and split of the depth.  256 x 256 tiles where they fill the device at least
+// once, else 128 x 128 ones; the depth is split where even those leave compute units
+// free, into parts of 256 depths or more.
+LinPlan sdm_linear_plan(int I, int J, int R, int ctype) {
     const int cus = sdm_device_simds() / 4;
-    const int64_t want = (2 * cus + tiles - 1) / std::max<int64_t>(tiles, 1), most = std::max(R / 256, 1);
-    return tiles * 2 > cus ? 1 : (int)std::max<int64_t>(1, std::min(want, most));
+    const auto tiles = [&](int64_t t) { return ((I + t - 1) / t) * ((J + t - 1) / t); };
+    LinPlan p{};
+    p.big = ctype == SDM_DT_BF16 && tiles(256) >= cus;
+    const int64_t n = std::max<int64_t>(p.big ? tiles(256) : tiles(128), 1);
+    const int64_t want = (2 * cus + n - 1) / n, most = std::max(R / 256, 1);
+    p.split = n * 2 > cus ? 1 : (int)std::max<int64_t>(1, std::min(want, most));
+    return p;
 }
 
 hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st) {
@@ -243,7 +428,8 @@ hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st) {
     if (g.ctype == SDM_DT_F32) e = launch_general<float, float, float>(g, st);
     else if (g.a.dtype == SDM_DT_F32) e = launch_general<bf16_t, float, bf16_t>(g, st);
     else if (g.b.dtype == SDM_DT_F32) e = launch_general<bf16_t, bf16_t, float>(g, st);
-    else e = launch_general<bf16_t, bf16_t, bf16_t>(g, st);
+    else if (g.big) e = launch_tile<256, 256, 2, 4>(g, st);
+    else e = launch_tile<128, 128, 2, 2>(g, st);
     if (e != hipSuccess || g.split <= 1) return e;
     const size_t n = (size_t)g.I * g.J;
     linear_join_kernel<<<(int)std::min<size_t>((n + 255) / 256, 8192), 256, 0, st>>>(g);

@@ -51,7 +51,8 @@ const char* too_large(int B, int T, int K, int N) {
 
 struct BwdWs {
     size_t dz, parts, split, total;
-    int ldz, split_x, split_w;
+    int ldz;
+    LinPlan px, pw;
     bool direct;   // dy is dz as it stands
 };
 BwdWs bwd_ws(int act, int dy_dtype, int w_dtype, int y_heads, int B, int T, int K, int N) {
@@ -59,8 +60,8 @@ BwdWs bwd_ws(int act, int dy_dtype, int w_dtype, int y_heads, int B, int T, int 
     const int M = B * T, m = w_dtype == SDM_BF16 ? 8 : 4;
     w.ldz = (N + m - 1) / m * m;
     w.direct = act == 0 && dy_dtype == w_dtype && y_heads == 0 && N % m == 0;
-    w.split_x = sdm_linear_split(M, K, N, w_dtype);
-    w.split_w = sdm_linear_split(N, K, M, w_dtype);
+    w.px = sdm_linear_plan(M, K, N, w_dtype);
+    w.pw = sdm_linear_plan(N, K, M, w_dtype);
     size_t o = 0;
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -69,8 +70,8 @@ BwdWs bwd_ws(int act, int dy_dtype, int w_dtype, int y_heads, int B, int T, int 
     };
     w.dz = take(w.direct ? 0 : (size_t)M * w.ldz * (w_dtype == SDM_BF16 ? 2 : 4));
     w.parts = take((size_t)sdm_linear_dz_parts(M) * N * 4);
-    w.split = take(std::max(w.split_x > 1 ? (size_t)w.split_x * M * K * 4 : 0,
-                            w.split_w > 1 ? (size_t)w.split_w * N * K * 4 : 0));
+    w.split = take(std::max(w.px.split > 1 ? (size_t)w.px.split * M * K * 4 : 0,
+                            w.pw.split > 1 ? (size_t)w.pw.split * N * K * 4 : 0));
     w.total = o;
     return w;
 }
@@ -81,7 +82,7 @@ extern "C" {
 
 size_t sdm_linear_workspace_bytes(int x_dtype, int w_dtype, int B, int T, int K, int N) {
     if (bad_sizes(x_dtype, 0, w_dtype, 0, B, T, K, N, 0) || too_large(B, T, K, N) || (int64_t)B * T == 0) return 0;
-    const int s = sdm_linear_split(B * T, N, K, w_dtype);
+    const int s = sdm_linear_plan(B * T, N, K, w_dtype).split;
     return s > 1 ? align256((size_t)s * B * T * N * 4) : 0;
 }
 
@@ -114,7 +115,9 @@ int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dty
     g.bias = bias;
     g.residual = residual;
     g.act = act;
-    g.split = sdm_linear_split(g.I, g.J, g.R, w_dtype);
+    const LinPlan pl = sdm_linear_plan(g.I, g.J, g.R, w_dtype);
+    g.split = pl.split;
+    g.big = pl.big;
     g.part = static_cast<float*>(workspace);
     SdmProfScope ps(SDM_K_LINEAR, (hipStream_t)stream);
     const hipError_t e = sdm_launch_linear(g, (hipStream_t)stream);
@@ -174,7 +177,8 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         g.R = N;
         g.ctype = w_dtype;
         g.out = lin_tokens(dx, x_dtype, B, T, K, x_heads);
-        g.split = L.split_x;
+        g.split = L.px.split;
+        g.big = L.px.big;
         g.part = split;
         e = sdm_launch_linear(g, st);
     }
@@ -188,7 +192,8 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         g.R = M;
         g.ctype = w_dtype;
         g.out = lin_flat(dw, w_dtype, N, K, K);
-        g.split = L.split_w;
+        g.split = L.pw.split;
+        g.big = L.pw.big;
         g.part = split;
         e = sdm_launch_linear(g, st);
     }
