@@ -28,7 +28,10 @@ struct LinGemm {
     LinMat a, b;
     bool ta, tb;
     int I, J, R;          // output rows, output columns, depth
-    int ctype;            // type the factors enter the matrix cores in
+    // 1, or 6: a and b hold three bf16 parts of fp32 values, `plane` values apart, and the
+    // products of parts of total order <= 2 are added up
+    int combos;
+    int64_t plane_a, plane_b;
     // out = act(C + bias) + residual, pre = C + bias; both laid out as `out`
     LinMat out;
     void* pre;
@@ -37,7 +40,7 @@ struct LinGemm {
     int act;
     // depth split over `split` workgroups: fp32 partial sums [split][I][J], added up by a second launch
     int split;
-    bool big;
+    bool big;             // 256 x 256 tiles, else 128 x 128
     float* part;
 };
 
@@ -45,11 +48,17 @@ struct LinPlan {
     bool big;
     int split;
 };
-LinPlan sdm_linear_plan(int I, int J, int R, int ctype);
+LinPlan sdm_linear_plan(int I, int J, int steps);
+// bf16 factors (or planes of parts) of any sizes
 hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st);
-// dz = dy act'(z) as rows [M][ldz] of ctype (zeros past N), and dbias = column sums of it
-// (through parts [nparts][N] added in order).
+// a with up to LIN_SKINNY rows, b [J, R], factors of any types; one launch
+#define LIN_SKINNY 64
+hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st);
+// an fp32 matrix as np bf16 planes [rows][ld] (np 1: rounded, 3: the parts), zeros past its end
+hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st);
+// dz = dy act'(z) as np planes [rows][ld], zeros past M and N, and dbias = its column sums
+// (through parts [sdm_linear_dz_parts(M)][N] added in order).  dz may be NULL.
 int sdm_linear_dz_parts(int M);
-hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int ctype, int ldz, void* dz,
-                                float* part, float* dbias, hipStream_t st);
+hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int np, int rows, int ld,
+                                void* dz, float* part, float* dbias, hipStream_t st);
 hipError_t sdm_launch_linear_zero(void* p, size_t words, hipStream_t st);

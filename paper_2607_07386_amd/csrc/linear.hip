@@ -7,6 +7,7 @@
 //   dw        C[n, k] = sum_m dz[m, n] x[m, k],   dbias[n] = sum_m dz[m, n]
 #include <algorithm>
 
+#include "gdn.h"
 #include "linear.h"
 #include "sdm_common.h"
 #include "sdm_internal.h"
@@ -25,6 +26,10 @@ __device__ __forceinline__ int64_t mat_col(const LinMat& m, int j) { return (int
 __device__ __forceinline__ uint16_t bf16_bits(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
 __device__ __forceinline__ void put(bf16_t* p, float x) { p->bits = bf16_bits(x); }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
+
+// us of a step of 64 depths (2048 x 2048 outputs, depth 16384, by the tile): a 256 x 256 tile,
+// and two 128 x 128 ones that share a compute unit
+constexpr double kStepBig = 2.1, kStepSmall = 1.7;
 
 constexpr float kSqrtHalf = 0.70710678118654752f, kInvSqrt2Pi = 0.39894228040143268f;
 __device__ __forceinline__ float lin_act(float z, int act) {
@@ -92,7 +97,10 @@ __device__ __forceinline__ bool lin_wide(const LinGemm& g) { return g.J % 8 == 0
 __device__ __forceinline__ void lin_store8(const LinGemm& g, bool wide, int64_t ro, int j, const float (&b)[8],
                                            float (&c)[8]) {
     if (!wide) {
-        for (int i = 0; i < 8 && j + i < g.J; ++i) lin_store(g, ro + mat_col(g.out, j + i), j + i, c[i]);
+        const bool flat = g.out.d == g.out.cols;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (j + i < g.J) lin_store(g, ro + (flat ? j + i : mat_col(g.out, j + i)), j + i, c[i]);
         return;
     }
     const int64_t o = ro + mat_col(g.out, j);
@@ -113,112 +121,6 @@ __device__ __forceinline__ void lin_store8(const LinGemm& g, bool wide, int64_t 
         for (int i = 0; i < 8; ++i) c[i] += r[i];
     }
     st8(const_cast<void*>(g.out.p), g.out.dtype, o, c);
-}
-
-// ---------------------------------------------------------------- general kernel
-// 128 x 128 x 32 tiles for any sizes, layouts and types: LDS rows are output
-// indices, so a factor stored depth-first is turned while it is staged.
-constexpr int GT = 128, GK = 32;
-template <typename CT>
-struct GenTile;
-template <>
-struct GenTile<bf16_t> {
-    static constexpr int LD = GK + 8, PIECE = 8;
-};
-template <>
-struct GenTile<float> {
-    static constexpr int LD = GK + 4, PIECE = 4;
-};
-
-// PIECE consecutive values along the matrix's columns, as CT (zeros outside)
-template <typename CT, typename ST>
-__device__ __forceinline__ void gen_load(const LinMat& m, int row, int col, CT (&x)[GenTile<CT>::PIECE]) {
-    constexpr int P = GenTile<CT>::PIECE;
-    const bool ok = row < m.rows && col < m.cols;
-    const ST* p = static_cast<const ST*>(m.p) + (ok ? mat_off(m, row, col) : 0);
-#pragma unroll
-    for (int i = 0; i < P; i += 4) {
-        const v4f v = ok ? ld4v(p + i) : v4zero();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) put(&x[i + j], v[j]);
-    }
-}
-
-template <typename CT, typename ST, bool TR>
-__device__ __forceinline__ void gen_stage(const LinMat& m, int o0, int r0, CT* lds) {
-    constexpr int P = GenTile<CT>::PIECE, LD = GenTile<CT>::LD;
-    constexpr int per_row = (TR ? GT : GK) / P, rows = TR ? GK : GT;
-    for (int u = threadIdx.x; u < rows * per_row; u += 256) {
-        const int r = u / per_row, c = u % per_row * P;
-        CT x[P];
-        gen_load<CT, ST>(m, (TR ? r0 : o0) + r, (TR ? o0 : r0) + c, x);
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            if constexpr (TR) lds[(c + i) * LD + r] = x[i];
-            else lds[r * LD + c + i] = x[i];
-        }
-    }
-}
-
-template <typename CT, typename AT, typename BT, bool TA, bool TB>
-__global__ __launch_bounds__(256) void linear_general_kernel(LinGemm g) {
-    constexpr int LD = GenTile<CT>::LD;
-    __shared__ __align__(16) CT sA[GT * LD], sB[GT * LD];
-    const int i0 = blockIdx.x * GT, j0 = blockIdx.y * GT;
-    const int lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
-    const int wi = (w >> 1) * 64, wj = (w & 1) * 64;
-    sdm_f32x4 acc[4][4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
-    const int steps = (g.R + GK - 1) / GK, per = (steps + g.split - 1) / g.split;
-    const int s0 = blockIdx.z * per, s1 = min(steps, s0 + per);
-    for (int s = s0; s < s1; ++s) {
-        gen_stage<CT, AT, TA>(g.a, i0, s * GK, sA);
-        gen_stage<CT, BT, TB>(g.b, j0, s * GK, sB);
-        __syncthreads();
-        if constexpr (sizeof(CT) == 2) {
-            sdm_bf16x8 fa[4], fb[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fa[i] = *reinterpret_cast<const sdm_bf16x8*>(sA + (wi + 16 * i + r16) * LD + 8 * q);
-                fb[i] = *reinterpret_cast<const sdm_bf16x8*>(sB + (wj + 16 * i + r16) * LD + 8 * q);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int k = 0; k < GK; k += 4) {
-                float fa[4], fb[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    fa[i] = sA[(wi + 16 * i + r16) * LD + k + q];
-                    fb[i] = sB[(wj + 16 * i + r16) * LD + k + q];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[i], fb[j], acc[i][j], 0, 0, 0);
-            }
-        }
-        __syncthreads();
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int oi = i0 + wi + 16 * i + 4 * q + r, oj = j0 + wj + 16 * j + r16;
-                if (oi >= g.I || oj >= g.J) continue;
-                if (g.split > 1) g.part[((size_t)blockIdx.z * g.I + oi) * g.J + oj] = acc[i][j][r];
-                else lin_store(g, mat_off(g.out, oi, oj), oj, acc[i][j][r]);
-            }
 }
 
 // The partial sums of a split depth, added in order, through the epilogue: eight
@@ -260,6 +162,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinGemm g) {
 // addresses, so the order is chosen by which piece a lane fetches).
 typedef float lin_f32x16 __attribute__((ext_vector_type(16)));
 typedef short lin_s4 __attribute__((ext_vector_type(4)));
+__device__ const uint4 lin_zeros = {0u, 0u, 0u, 0u};   // what pieces outside a matrix read
 
 constexpr int BK = 64;
 constexpr uint32_t LIN_OUT = 0x80000000u;   // offset of what lies outside a matrix: loads of it give zeros
@@ -271,18 +174,24 @@ __device__ __forceinline__ void dma16(__amdgpu_buffer_rsrc_t r, uint32_t off, vo
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)l, 16, (int)off, 0, 0, 0);
 }
 
+__device__ __forceinline__ void dma16g(const void* g, void* l) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)g,
+                                     (__attribute__((address_space(3))) void*)l, 16, 0, 0);
+}
+
 // A factor's tile: O output indices x 64 depths.  Each of the NW waves moves O / (8 NW)
-// runs of 1 KB.  A lane's places are 32-bit byte offsets from a base that moves along
-// the depth, so that a step costs no vector arithmetic where the depth runs evenly
-// (offsets_fit() says whether they do; EVEN: 64 depths always follow one another).
+// runs of 1 KB.  EVEN: 64 depths always follow one another and a lane's places are
+// 32-bit byte offsets from a base that moves along the depth, so that a step costs
+// no vector arithmetic.  Otherwise a lane forms its addresses at every step.
 template <int O, int NW, bool TR, bool EVEN>
 struct LinTile {
     static constexpr int RUNS = O / (8 * NW);
     static constexpr int PPR = (TR ? O : BK) / 8;      // pieces of a row of the tile in LDS
     static constexpr int RPR = 64 / PPR;               // rows of a run
     static constexpr int MASK = PPR / 4 - 1;           // TR: 4 pieces (32 outputs) move together
-    const bf16_t* base;      // !TR: start of the first row's sequence; TR: of the matrix
-    uint32_t off[RUNS];      // !TR: the lane's rows; TR: the lane's columns
+    const bf16_t* base;      // EVEN, !TR: start of the first row's sequence; else of the matrix
+    uint32_t off[RUNS];      // EVEN: the lane's rows (!TR) or columns (TR)
+    const bf16_t* at[RUNS];  // !EVEN, !TR: the lane's rows (NULL past the end)
 
     __device__ __forceinline__ static int swz(int r) { return TR ? 4 * (r & MASK) : r & 7; }
     __device__ __forceinline__ static int run0() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RUNS; }
@@ -292,7 +201,7 @@ struct LinTile {
 
     __device__ __forceinline__ void init(const LinMat& m, int o0) {
         base = static_cast<const bf16_t*>(m.p);
-        if constexpr (!TR) {
+        if constexpr (EVEN && !TR) {
             const int seq = o0 / m.T;
             base += (int64_t)seq * m.sb;
 #pragma unroll
@@ -300,42 +209,45 @@ struct LinTile {
                 const int o = o0 + (run0() + i) * RPR + row();
                 off[i] = o < m.rows ? (uint32_t)((int64_t)(o / m.T - seq) * m.sb + (int64_t)(o % m.T) * m.st) * 2 : LIN_OUT;
             }
-        } else {
+        } else if constexpr (EVEN) {
 #pragma unroll
             for (int i = 0; i < RUNS; ++i) {
                 const int c = o0 + piece((run0() + i) * RPR + row()) * 8;
                 off[i] = c < m.cols ? (uint32_t)mat_col(m, c) * 2 : LIN_OUT;
             }
+        } else if constexpr (!TR) {
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i) {
+                const int o = o0 + (run0() + i) * RPR + row();
+                at[i] = o < m.rows ? base + mat_row(m, o) : nullptr;
+            }
         }
     }
-    __device__ __forceinline__ void fetch(const LinMat& m, int r0, unsigned char* lds) {
-        if constexpr (!TR) {
-            if constexpr (EVEN) {
-                const auto buf = lin_buf(base + mat_col(m, r0));
-                const uint32_t pc = piece(row()) * 16;
+    // the tile at depths r0 .. r0 + 63 of the plane `plane` values into the matrix
+    __device__ __forceinline__ void fetch(const LinMat& m, int o0, int r0, int64_t plane, unsigned char* lds) {
+        if constexpr (EVEN && !TR) {
+            const auto buf = lin_buf(base + plane + mat_col(m, r0));
+            const uint32_t pc = piece(row()) * 16;
 #pragma unroll
-                for (int i = 0; i < RUNS; ++i) dma16(buf, off[i] + pc, lds + (run0() + i) * 1024);
-            } else {
-                const int c = r0 + piece(row()) * 8;
-                const uint32_t o = c < m.cols ? (uint32_t)mat_col(m, c) * 2 : LIN_OUT;
+            for (int i = 0; i < RUNS; ++i) dma16(buf, off[i] + pc, lds + (run0() + i) * 1024);
+        } else if constexpr (EVEN) {
+            const auto buf = lin_buf(base + plane + mat_row(m, r0));
 #pragma unroll
-                for (int i = 0; i < RUNS; ++i) dma16(lin_buf(base), (off[i] | o) & LIN_OUT ? LIN_OUT : off[i] + o, lds + (run0() + i) * 1024);
-            }
+            for (int i = 0; i < RUNS; ++i)
+                dma16(buf, off[i] + ((run0() + i) * RPR + row()) * (uint32_t)m.st * 2, lds + (run0() + i) * 1024);
+        } else if constexpr (!TR) {
+            const int c = r0 + piece(row()) * 8;
+            const bool ok = c < m.cols;
+            const int64_t co = ok ? plane + mat_col(m, c) : 0;
+#pragma unroll
+            for (int i = 0; i < RUNS; ++i)
+                dma16g(at[i] && ok ? (const void*)(at[i] + co) : (const void*)&lin_zeros, lds + (run0() + i) * 1024);
         } else {
-            const int seq = r0 / m.T;
-            const auto buf = lin_buf(base + (int64_t)seq * m.sb + (int64_t)(r0 - seq * m.T) * m.st);
-            if constexpr (EVEN) {
 #pragma unroll
-                for (int i = 0; i < RUNS; ++i)
-                    dma16(buf, off[i] + ((run0() + i) * RPR + row()) * (uint32_t)m.st * 2, lds + (run0() + i) * 1024);
-            } else {
-#pragma unroll
-                for (int i = 0; i < RUNS; ++i) {
-                    const int kr = (run0() + i) * RPR + row(), t = r0 - seq * m.T + kr;
-                    const int64_t o = (int64_t)(t / m.T) * m.sb + (int64_t)(t % m.T - (r0 - seq * m.T)) * m.st;
-                    const uint32_t at = off[i] + (uint32_t)((int)o * 2);
-                    dma16(buf, r0 + kr < m.rows && !(off[i] & LIN_OUT) ? at : LIN_OUT, lds + (run0() + i) * 1024);
-                }
+            for (int i = 0; i < RUNS; ++i) {
+                const int kr = (run0() + i) * RPR + row(), r = r0 + kr, c = o0 + piece(kr) * 8;
+                dma16g(r < m.rows && c < m.cols ? (const void*)(base + plane + mat_off(m, r, c)) : (const void*)&lin_zeros,
+                       lds + (run0() + i) * 1024);
             }
         }
     }
@@ -390,15 +302,19 @@ __global__ __launch_bounds__(WR* WC * 64) void linear_tile_kernel(LinGemm g, int
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    const int steps = (g.R + BK - 1) / BK, per = (steps + g.split - 1) / g.split;
+    const int depth = (g.R + BK - 1) / BK, steps = depth * g.combos, per = (steps + g.split - 1) / g.split;
     const int s0 = blockIdx.y * per, s1 = min(steps, s0 + per);
     TileA ta;
     TileB tb;
     ta.init(g.a, i0);
     tb.init(g.b, j0);
     const auto fetch = [&](int s, unsigned char* la, unsigned char* lb) {
-        ta.fetch(g.a, s * BK, la);
-        tb.fetch(g.b, s * BK, lb);
+        // fp32 factors: the products of parts of total order <= 2, smallest first
+        // (parts (0,2) (1,1) (2,0) (0,1) (1,0) (0,0), two bits each)
+        const int c = g.combos > 1 ? s / depth : 5, r0 = (g.combos > 1 ? s - c * depth : s) * BK;
+        const int pa = (0x124 >> 2 * c) & 3, pb = (0x46 >> 2 * c) & 3;
+        ta.fetch(g.a, i0, r0, pa * g.plane_a, la);
+        tb.fetch(g.b, j0, r0, pb * g.plane_b, lb);
     };
     // fragments one step of 16 depths ahead; the fences keep the scheduler from
     // reading the whole tile ahead, which would spill
@@ -491,47 +407,199 @@ hipError_t launch_tile(const LinGemm& g, hipStream_t st) {
     else linear_tile_kernel<BM, BN, WR, WC, true, true, EVEN><<<grid, WR * WC * 64, 0, st>>>(g, tj);
     return hipGetLastError();
 }
-// whether every 64 depths of a factor follow one another in memory
+
+// Whether every 64 depths of a factor follow one another in memory, up to a multiple of
+// 64, and 32-bit offsets reach a tile from the start of its first row's sequence.
 bool even_depth(const LinMat& m, bool tr, int R) {
-    return R % BK == 0 && (tr ? m.T == m.rows || m.T % BK == 0 : m.d == m.cols || m.d % BK == 0);
+    const int up = (R + BK - 1) / BK * BK, span = tr ? BK : 256;
+    const bool flat = m.T == m.rows;
+    const int64_t reach = flat ? (int64_t)span * m.st + m.cols : (int64_t)(span / m.T + 2) * m.sb;
+    if (reach * 2 >= (int64_t)1 << 31) return false;
+    return tr ? m.rows >= up && (flat || m.T % BK == 0) : m.cols >= up && (m.d == m.cols || m.d % BK == 0);
 }
 
-// ---------------------------------------------------------------- dz, dbias
-// A workgroup takes 64 columns x `rows` rows: 16 columns-of-four lanes x 16 rows at a time.
-constexpr int DZ_ROWS = 256;
-template <typename CT>
-__global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z, int z_dtype, int act, int ldz,
-                                                        CT* dz, float* part) {
-    __shared__ float red[4][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), rg = threadIdx.x >> 6;
-    const int m0 = blockIdx.y * DZ_ROWS, m1 = min(dy.rows, m0 + DZ_ROWS);
-    float sum = 0.f;
-    if (c < ldz) {
-        const bool ok = c < dy.cols;
-        const int64_t co = ok ? mat_col(dy, c) : 0;
-        for (int m = m0 + rg; m < m1; m += 4) {
-            float v = 0.f;
-            if (ok) {
-                const int64_t o = mat_row(dy, m) + co;
-                v = ld_any(dy.p, dy.dtype, o);
-                if (act) v *= lin_act_slope(ld_any(z, z_dtype, o), act);
-                sum += v;
+// ---------------------------------------------------------------- few rows
+// Up to 64 rows of x (the decode step): bound by reading w once.  A workgroup holds 16
+// outputs; its 8 waves take the depth in turns of 64 (a row's 128-byte line in bf16)
+// and their sums meet in LDS, so a call is one launch.
+// eight depths of a row, from offsets o0 and o1 (the second four, which may be another
+// head's); zeros where the depth has ended
+template <int NT>
+__device__ __forceinline__ GdnFrag<NT> skinny_frag(const float* row, int64_t o0, int64_t o1, bool ok0, bool ok1) {
+    const v4f a = v4sel(ok0, ld4(row + o0), v4zero()), b = v4sel(ok1, ld4(row + o1), v4zero());
+    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    if constexpr (NT == 3) {
+        return gdn_split(x);
+    } else {
+        GdnFrag<1> f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.t[0][i] = (__bf16)x[i];
+        return f;
+    }
+}
+template <int NT>
+__device__ __forceinline__ GdnFrag<NT> skinny_frag(const bf16_t* row, int64_t o0, int64_t, bool ok0, bool) {
+    u4v v = *reinterpret_cast<const u4v*>(row + o0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = ok0 ? v[i] : 0u;
+    GdnFrag<NT> f;
+    f.t[0] = __builtin_bit_cast(sdm_bf16x8, v);
+    return f;
+}
+
+template <typename WT, typename XT, int MT, bool FLAT>
+__global__ __launch_bounds__(512) void linear_skinny_kernel(LinGemm g) {
+    constexpr int NT = sizeof(WT) == 4 ? 3 : 1;
+    __shared__ float red[8][MT][256];
+    const int j0 = blockIdx.x * 16, lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+    // rows past the end repeat the last one: what they give is not stored
+    const WT* wp = static_cast<const WT*>(g.b.p) + (size_t)min(j0 + r16, g.J - 1) * g.R;
+    const XT* xp[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) xp[m] = static_cast<const XT*>(g.a.p) + mat_row(g.a, min(16 * m + r16, g.I - 1));
+    sdm_f32x4 acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k0 = w * 64; k0 < g.R; k0 += 512) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + 32 * h + 8 * q;
+            const bool ok0 = k < g.R, ok1 = k + 4 < g.R;
+            const int ka = ok0 ? k : 0, kb = ok1 ? k + 4 : 0;
+            const GdnFrag<NT> fw = skinny_frag<NT>(wp, ka, kb, ok0, ok1);
+            const int64_t xa = FLAT ? ka : mat_col(g.a, ka), xb = FLAT ? kb : mat_col(g.a, kb);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m] = gdn_mm(skinny_frag<NT>(xp[m], xa, xb, ok0, ok1), fw, acc[m]);
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) red[w][m][(4 * q + r) * 16 + r16] = acc[m][r];
+    __syncthreads();
+    for (int u = threadIdx.x; u < MT * 256; u += 512) {
+        float c = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c += red[i][u >> 8][u & 255];
+        const int oi = u >> 4, oj = j0 + (u & 15);
+        if (oi < g.I && oj < g.J) lin_store(g, mat_off(g.out, oi, oj), oj, c);
+    }
+}
+
+template <typename WT, typename XT, bool FLAT>
+hipError_t launch_skinny_rows(const LinGemm& g, hipStream_t st) {
+    const int grid = (g.J + 15) / 16;
+    if (g.I <= 16) linear_skinny_kernel<WT, XT, 1, FLAT><<<grid, 512, 0, st>>>(g);
+    else if (g.I <= 32) linear_skinny_kernel<WT, XT, 2, FLAT><<<grid, 512, 0, st>>>(g);
+    else linear_skinny_kernel<WT, XT, 4, FLAT><<<grid, 512, 0, st>>>(g);
+    return hipGetLastError();
+}
+template <typename WT, typename XT>
+hipError_t launch_skinny(const LinGemm& g, hipStream_t st) {
+    return g.a.d == g.a.cols ? launch_skinny_rows<WT, XT, true>(g, st) : launch_skinny_rows<WT, XT, false>(g, st);
+}
+
+// ---------------------------------------------------------------- parts, dz, dbias
+// NP = 1: rounded to bf16; NP = 3: the three bf16 parts of an fp32 value.
+template <int NP>
+__device__ __forceinline__ void put_parts(bf16_t* p, int64_t plane, const float (&x)[8]) {
+    if constexpr (NP == 1) {
+        st8(p, SDM_DT_BF16, 0, x);
+    } else {
+        const GdnFrag<3> f = gdn_split(x);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<sdm_bf16x8*>(p + i * plane) = f.t[i];
+    }
+}
+
+// An fp32 matrix as bf16 planes [rows][ld], zeros past its end (both multiples of 64).
+template <int NP>
+__global__ __launch_bounds__(256) void linear_parts_kernel(LinMat m, int rows, int ld, bf16_t* out, int64_t plane) {
+    const int c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
+    if (c >= ld) return;
+    const float* src = static_cast<const float*>(m.p);
+    const int64_t o0 = c < m.cols ? mat_col(m, c) : 0, o1 = c + 4 < m.cols ? mat_col(m, c + 4) : 0;
+    for (int r = blockIdx.y * 8 + (threadIdx.x >> 5); r < rows; r += gridDim.y * 8) {
+        float x[8];
+        const int64_t ro = r < m.rows ? mat_row(m, r) : 0;
+        const v4f a = r < m.rows && c < m.cols ? ld4(src + ro + o0) : v4zero();
+        const v4f b = r < m.rows && c + 4 < m.cols ? ld4(src + ro + o1) : v4zero();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = a[i];
+            x[4 + i] = b[i];
+        }
+        put_parts<NP>(out + (int64_t)r * ld + c, plane, x);
+    }
+}
+
+// dz = dy act'(z) as planes [rows][ld] (zeros past M and N) and its column sums over this
+// workgroup's rows: eight columns a thread, 8 rows at a time.
+constexpr int DZ_ROWS = 128;
+template <int NP>
+__global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z, int z_dtype, int act, int rows,
+                                                        int ld, bf16_t* dz, int64_t plane, float* part) {
+    __shared__ float red[8][256];
+    const int cl = threadIdx.x & 31, rg = threadIdx.x >> 5, c = (blockIdx.x * 32 + cl) * 8;
+    const bool wide = dy.cols % 8 == 0 && dy.d % 8 == 0;
+    int64_t cols[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) cols[i] = c + i < dy.cols ? mat_col(dy, c + i) : 0;
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (c < ld) {
+        const int m1 = min(rows, (int)(blockIdx.y + 1) * DZ_ROWS);
+        for (int m = blockIdx.y * DZ_ROWS + rg; m < m1; m += 8) {
+            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (m < dy.rows && c < dy.cols) {
+                const int64_t ro = mat_row(dy, m);
+                if (wide) {
+                    ld8(dy.p, dy.dtype, ro + cols[0], x);
+                    if (act) {
+                        float zz[8];
+                        ld8(z, z_dtype, ro + cols[0], zz);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] *= act == 1 ? lin_act_slope(zz[i], 1) : lin_act_slope(zz[i], 2);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int64_t o = ro + cols[i];   // a column past the end reads the first one
+                        x[i] = ld_any(dy.p, dy.dtype, o);
+                        if (act) x[i] *= lin_act_slope(ld_any(z, z_dtype, o), act);
+                        x[i] = c + i < dy.cols ? x[i] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += x[i];
             }
-            if (dz) put(dz + (size_t)m * ldz + c, v);
+            if (dz) put_parts<NP>(dz + (int64_t)m * ld + c, plane, x);
         }
     }
     if (!part) return;
-    red[rg][threadIdx.x & 63] = sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) red[rg][cl * 8 + i] = sum[i];
     __syncthreads();
-    if (rg == 0 && c < dy.cols)
-        part[(size_t)blockIdx.y * dy.cols + c] =
-            red[0][threadIdx.x] + red[1][threadIdx.x] + red[2][threadIdx.x] + red[3][threadIdx.x];
+    const int n = blockIdx.x * 256 + threadIdx.x;
+    if (n < dy.cols) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += red[i][threadIdx.x];
+        part[(size_t)blockIdx.y * dy.cols + n] = s;
+    }
 }
+// 32 columns a workgroup, its eight groups of threads taking the parts in turn
 __global__ __launch_bounds__(256) void linear_colsum_kernel(const float* part, int parts, int N, float* out) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= N) return;
+    __shared__ float red[8][32];
+    const int cl = threadIdx.x & 31, rg = threadIdx.x >> 5, c = blockIdx.x * 32 + cl;
     float s = 0.f;
-    for (int p = 0; p < parts; ++p) s += part[(size_t)p * N + c];
+    if (c < N)
+        for (int p = rg; p < parts; p += 8) s += part[(size_t)p * N + c];
+    red[rg][cl] = s;
+    __syncthreads();
+    if (rg || c >= N) return;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += red[i][cl];
     out[c] = s;
 }
 
@@ -539,71 +607,67 @@ __global__ __launch_bounds__(256) void linear_zero_kernel(uint32_t* p, size_t n)
     for (size_t u = (size_t)blockIdx.x * 256 + threadIdx.x; u < n; u += (size_t)gridDim.x * 256) p[u] = 0u;
 }
 
-template <typename CT, typename AT, typename BT>
-hipError_t launch_general(const LinGemm& g, hipStream_t st) {
-    const dim3 grid((g.I + GT - 1) / GT, (g.J + GT - 1) / GT, g.split);
-    if (!g.ta && !g.tb) linear_general_kernel<CT, AT, BT, false, false><<<grid, 256, 0, st>>>(g);
-    else if (!g.ta) linear_general_kernel<CT, AT, BT, false, true><<<grid, 256, 0, st>>>(g);
-    else linear_general_kernel<CT, AT, BT, true, true><<<grid, 256, 0, st>>>(g);
-    return hipGetLastError();
-}
-
 }  // namespace
 
-namespace {
-// Whether the tiled kernel's 32-bit offsets reach a tile of this factor: rows of `span`
-// tokens (and the columns with them) from the start of the first one's sequence.
-bool offsets_fit(const LinMat& m, int span) {
-    const int64_t seq = m.T == m.rows ? (int64_t)span * m.st + m.cols : (int64_t)(span / m.T + 2) * m.sb;
-    return seq * 2 < (int64_t)1 << 31;
-}
-bool tiled(const LinGemm& g) {
-    return g.ctype == SDM_DT_BF16 && g.a.dtype == SDM_DT_BF16 && g.b.dtype == SDM_DT_BF16 &&
-           offsets_fit(g.a, 256) && offsets_fit(g.b, 256);
-}
-}  // namespace
-
-// Tile and split of the depth.  256 x 256 tiles where they fill the device at least
-// once, else 128 x 128 ones; the depth is split where even those leave compute units
-// free, into parts of 256 depths or more.
-LinPlan sdm_linear_plan(int I, int J, int R, int ctype) {
+// Tile and split of the depth (`steps` of 64), by the time they take: a 256 x 256 tile has
+// a compute unit to itself, two 128 x 128 ones share it; a split depth is joined by a pass
+// over the partial sums.
+LinPlan sdm_linear_plan(int I, int J, int steps) {
     const int cus = sdm_device_simds() / 4;
-    const auto tiles = [&](int64_t t) { return ((I + t - 1) / t) * ((J + t - 1) / t); };
-    LinPlan p{};
-    p.big = ctype == SDM_DT_BF16 && tiles(256) >= cus;
-    const int64_t n = std::max<int64_t>(p.big ? tiles(256) : tiles(128), 1);
-    const int64_t want = (2 * cus + n - 1) / n, most = std::max(R / 256, 1);
-    p.split = n * 2 > cus ? 1 : (int)std::max<int64_t>(1, std::min(want, most));
-    return p;
+    LinPlan best{};
+    double t_best = 1e30;
+    for (int big = 0; big < 2; ++big) {
+        const int t = big ? 256 : 128;
+        const int64_t n = (int64_t)((I + t - 1) / t) * ((J + t - 1) / t);
+        for (int split = 1; split <= 64 && (split == 1 || steps / split >= 4); split *= 2) {
+            const int64_t slots = (int64_t)cus * (big ? 1 : 2), turns = (n * split + slots - 1) / slots;
+            double us = turns * (steps + split - 1) / split * (big ? kStepBig : kStepSmall) + (big ? 6.0 : 4.0);
+            if (split > 1) us += 4.0 + (double)I * J * split * 8 / 4e6;
+            if (us < t_best) {
+                t_best = us;
+                best.big = big;
+                best.split = split;
+            }
+        }
+    }
+    return best;
 }
 
 hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st) {
+    const bool even = even_depth(g.a, g.ta, g.R) && even_depth(g.b, g.tb, g.R);
     hipError_t e;
-    if (g.ctype == SDM_DT_F32) e = launch_general<float, float, float>(g, st);
-    else if (g.a.dtype == SDM_DT_F32) e = launch_general<bf16_t, float, bf16_t>(g, st);
-    else if (g.b.dtype == SDM_DT_F32) e = launch_general<bf16_t, bf16_t, float>(g, st);
-    else if (!tiled(g)) e = launch_general<bf16_t, bf16_t, bf16_t>(g, st);
-    else {
-        const bool even = even_depth(g.a, g.ta, g.R) && even_depth(g.b, g.tb, g.R);
-        if (g.big) e = even ? launch_tile<256, 256, 2, 4, true>(g, st) : launch_tile<256, 256, 2, 4, false>(g, st);
-        else e = even ? launch_tile<128, 128, 2, 2, true>(g, st) : launch_tile<128, 128, 2, 2, false>(g, st);
-    }
+    if (g.big) e = even ? launch_tile<256, 256, 2, 4, true>(g, st) : launch_tile<256, 256, 2, 4, false>(g, st);
+    else e = even ? launch_tile<128, 128, 2, 2, true>(g, st) : launch_tile<128, 128, 2, 2, false>(g, st);
     if (e != hipSuccess || g.split <= 1) return e;
     linear_join_kernel<<<dim3((g.J + 255) / 256, std::min((g.I + 7) / 8, 4096)), 256, 0, st>>>(g);
     return hipGetLastError();
 }
 
-int sdm_linear_dz_parts(int M) { return (M + DZ_ROWS - 1) / DZ_ROWS; }
+hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st) {
+    if (g.b.dtype == SDM_DT_F32) return launch_skinny<float, float>(g, st);
+    if (g.a.dtype == SDM_DT_F32) return launch_skinny<bf16_t, float>(g, st);
+    return launch_skinny<bf16_t, bf16_t>(g, st);
+}
 
-hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int ctype, int ldz, void* dz,
-                                float* part, float* dbias, hipStream_t st) {
-    const int parts = sdm_linear_dz_parts(dy.rows);
-    const dim3 grid((ldz + 63) / 64, parts);
+hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st) {
+    const dim3 grid((ld + 255) / 256, std::min((rows + 7) / 8, 2048));
+    if (np == 3) linear_parts_kernel<3><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
+    else linear_parts_kernel<1><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
+    return hipGetLastError();
+}
+
+int sdm_linear_dz_parts(int M) { return (M + 63) / 64 * 64 / DZ_ROWS + 1; }
+
+hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int np, int rows, int ld,
+                                void* dz, float* part, float* dbias, hipStream_t st) {
+    const int parts = (rows + DZ_ROWS - 1) / DZ_ROWS;
+    const dim3 grid((ld + 255) / 256, parts);
     float* p = dbias ? part : nullptr;
-    if (ctype == SDM_DT_F32)
-        linear_dz_kernel<float><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, ldz, static_cast<float*>(dz), p);
-    else linear_dz_kernel<bf16_t><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, ldz, static_cast<bf16_t*>(dz), p);
-    if (dbias) linear_colsum_kernel<<<(dy.cols + 255) / 256, 256, 0, st>>>(part, parts, dy.cols, dbias);
+    bf16_t* o = static_cast<bf16_t*>(dz);
+    const int64_t plane = (int64_t)rows * ld;
+    if (np == 3) linear_dz_kernel<3><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, rows, ld, o, plane, p);
+    else linear_dz_kernel<1><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, rows, ld, o, plane, p);
+    if (dbias) linear_colsum_kernel<<<(dy.cols + 31) / 32, 256, 0, st>>>(part, parts, dy.cols, dbias);
     return hipGetLastError();
 }
 

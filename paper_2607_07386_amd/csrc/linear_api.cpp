@@ -49,32 +49,54 @@ const char* too_large(int B, int T, int K, int N) {
     return nullptr;
 }
 
-struct BwdWs {
-    size_t dz, parts, split, total;
-    int ldz;
-    LinPlan px, pw;
-    bool direct;   // dy is dz as it stands
-};
-BwdWs bwd_ws(int act, int dy_dtype, int w_dtype, int y_heads, int B, int T, int K, int N) {
-    BwdWs w{};
-    const int M = B * T, m = w_dtype == SDM_BF16 ? 8 : 4;
-    w.ldz = (N + m - 1) / m * m;
-    w.direct = act == 0 && dy_dtype == w_dtype && y_heads == 0 && N % m == 0;
-    w.px = sdm_linear_plan(M, K, N, w_dtype);
-    w.pw = sdm_linear_plan(N, K, M, w_dtype);
-    size_t o = 0;
-    auto take = [&](size_t bytes) {
-        const size_t at = o;
-        o += align256(bytes);
+int up64(int x) { return (x + 63) / 64 * 64; }
+int parts_of(int w_dtype) { return w_dtype == SDM_F32 ? 3 : 1; }
+int combos_of(int w_dtype) { return w_dtype == SDM_F32 ? 6 : 1; }
+int steps_of(int R, int w_dtype) { return (R + 63) / 64 * combos_of(w_dtype); }
+
+// Offsets into a call's workspace.  fp32 factors enter the products as bf16 planes,
+// padded to multiples of 64 both ways.
+struct Ws {
+    size_t x = 0, w = 0, dz = 0, parts = 0, split = 0, total = 0;
+    LinPlan py{}, px{}, pw{};
+    bool direct = false;   // dy is dz as it stands
+    size_t take(size_t bytes) {
+        const size_t at = total;
+        total += align256(bytes);
         return at;
-    };
-    w.dz = take(w.direct ? 0 : (size_t)M * w.ldz * (w_dtype == SDM_BF16 ? 2 : 4));
-    w.parts = take((size_t)sdm_linear_dz_parts(M) * N * 4);
-    w.split = take(std::max(w.px.split > 1 ? (size_t)w.px.split * M * K * 4 : 0,
-                            w.pw.split > 1 ? (size_t)w.pw.split * N * K * 4 : 0));
-    w.total = o;
-    return w;
+    }
+};
+size_t planes(int np, int rows, int cols) { return (size_t)np * up64(rows) * up64(cols) * 2; }
+size_t split_bytes(const LinPlan& p, int I, int J) { return p.split > 1 ? (size_t)p.split * I * J * 4 : 0; }
+
+Ws fwd_ws(int x_dtype, int w_dtype, int M, int K, int N) {
+    Ws s;
+    if (M <= LIN_SKINNY) return s;
+    if (x_dtype == SDM_F32) s.x = s.take(planes(parts_of(w_dtype), M, K));
+    if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
+    s.py = sdm_linear_plan(M, N, steps_of(K, w_dtype));
+    s.split = s.take(split_bytes(s.py, M, N));
+    return s;
 }
+Ws bwd_ws(int x_dtype, int w_dtype, int act, int dy_dtype, int y_heads, int M, int K, int N) {
+    Ws s;
+    const int np = parts_of(w_dtype);
+    s.direct = w_dtype == SDM_BF16 && act == 0 && dy_dtype == SDM_BF16 && y_heads == 0 && N % 8 == 0;
+    if (!s.direct) s.dz = s.take(planes(np, M, N));
+    if (x_dtype == SDM_F32) s.x = s.take(planes(np, M, K));
+    if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
+    s.parts = s.take((size_t)sdm_linear_dz_parts(M) * N * 4);
+    s.px = sdm_linear_plan(M, K, steps_of(N, w_dtype));
+    s.pw = sdm_linear_plan(N, K, steps_of(M, w_dtype));
+    s.split = s.take(std::max(split_bytes(s.px, M, K), split_bytes(s.pw, N, K)));
+    return s;
+}
+// planes of a rows x cols matrix: as rows of a factor (depth = columns), or depth first
+LinMat plane_mat(const void* p, int rows, int cols, bool depth_rows) {
+    LinMat m = lin_flat(p, SDM_BF16, depth_rows ? up64(rows) : rows, depth_rows ? cols : up64(cols), up64(cols));
+    return m;
+}
+int64_t plane_len(int rows, int cols) { return (int64_t)up64(rows) * up64(cols); }
 
 }  // namespace
 
@@ -82,8 +104,7 @@ extern "C" {
 
 size_t sdm_linear_workspace_bytes(int x_dtype, int w_dtype, int B, int T, int K, int N) {
     if (bad_sizes(x_dtype, 0, w_dtype, 0, B, T, K, N, 0) || too_large(B, T, K, N) || (int64_t)B * T == 0) return 0;
-    const int s = sdm_linear_plan(B * T, N, K, w_dtype).split;
-    return s > 1 ? align256((size_t)s * B * T * N * 4) : 0;
+    return fwd_ws(x_dtype, w_dtype, B * T, K, N).total;
 }
 
 int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const float* bias, int act,
@@ -103,24 +124,43 @@ int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dty
         return fail(SDM_ERR_INVALID_ARG, "misaligned pointer (16-byte alignment required)");
     const int rc = check_ws(workspace, ws_bytes, sdm_linear_workspace_bytes(x_dtype, w_dtype, B, T, K, N));
     if (rc != SDM_OK) return rc;
+    const int M = B * T;
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
+    hipStream_t st = (hipStream_t)stream;
     LinGemm g{};
     g.a = lin_tokens(x, x_dtype, B, T, K, x_heads);
     g.b = lin_flat(w, w_dtype, N, K, K);
-    g.I = B * T;
+    g.I = M;
     g.J = N;
     g.R = K;
-    g.ctype = w_dtype;
+    g.combos = combos_of(w_dtype);
     g.out = lin_tokens(y, y_dtype, B, T, N, y_heads);
     g.pre = z;
     g.bias = bias;
     g.residual = residual;
     g.act = act;
-    const LinPlan pl = sdm_linear_plan(g.I, g.J, g.R, w_dtype);
-    g.split = pl.split;
-    g.big = pl.big;
-    g.part = static_cast<float*>(workspace);
-    SdmProfScope ps(SDM_K_LINEAR, (hipStream_t)stream);
-    const hipError_t e = sdm_launch_linear(g, (hipStream_t)stream);
+    g.split = 1;
+    SdmProfScope ps(SDM_K_LINEAR, st);
+    hipError_t e = hipSuccess;
+    if (M <= LIN_SKINNY) {
+        e = sdm_launch_linear_skinny(g, st);
+        return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear launch");
+    }
+    const Ws L = fwd_ws(x_dtype, w_dtype, M, K, N);
+    if (x_dtype == SDM_F32) {
+        e = sdm_launch_linear_parts(g.a, parts_of(w_dtype), up64(M), up64(K), ws + L.x, st);
+        g.a = plane_mat(ws + L.x, M, K, false);
+        g.plane_a = plane_len(M, K);
+    }
+    if (e == hipSuccess && w_dtype == SDM_F32) {
+        e = sdm_launch_linear_parts(g.b, 3, up64(N), up64(K), ws + L.w, st);
+        g.b = plane_mat(ws + L.w, N, K, false);
+        g.plane_b = plane_len(N, K);
+    }
+    g.split = L.py.split;
+    g.big = L.py.big;
+    g.part = reinterpret_cast<float*>(ws + L.split);
+    if (e == hipSuccess) e = sdm_launch_linear(g, st);
     return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear launch");
 }
 
@@ -128,7 +168,7 @@ size_t sdm_linear_bwd_workspace_bytes(int x_dtype, int w_dtype, int act, int dy_
                                       int y_heads) {
     if (bad_sizes(x_dtype, 0, w_dtype, act, B, T, K, N, y_heads) || too_large(B, T, K, N) || (int64_t)B * T == 0)
         return 0;
-    return bwd_ws(act, dy_dtype, w_dtype, y_heads, B, T, K, N).total;
+    return bwd_ws(x_dtype, w_dtype, act, dy_dtype, y_heads, B * T, K, N).total;
 }
 
 int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const void* z, int z_dtype,
@@ -156,46 +196,52 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         if (e == hipSuccess && dbias) e = sdm_launch_linear_zero(dbias, N, st);
         return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear_bwd launch");
     }
-    const BwdWs L = bwd_ws(act, dy_dtype, w_dtype, y_heads, B, T, K, N);
+    const Ws L = bwd_ws(x_dtype, w_dtype, act, dy_dtype, y_heads, M, K, N);
     const int rc = check_ws(workspace, ws_bytes, L.total);
     if (rc != SDM_OK) return rc;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
-    float* split = reinterpret_cast<float*>(ws + L.split);
+    const int np = parts_of(w_dtype);
     SdmProfScope ps(SDM_K_LINEAR, st);
     if (!L.direct || dbias)
-        e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_dtype, act, w_dtype, L.ldz,
+        e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_dtype, act, np, up64(M), up64(N),
                                  L.direct ? nullptr : ws + L.dz, reinterpret_cast<float*>(ws + L.parts), dbias, st);
-    const LinMat dz = L.direct ? lin_flat(dy, w_dtype, M, N, N) : lin_flat(ws + L.dz, w_dtype, M, N, L.ldz);
-    const LinMat xm = lin_tokens(x, x_dtype, B, T, K, x_heads);
+    LinGemm g{};
+    g.combos = combos_of(w_dtype);
+    g.tb = true;
+    g.part = reinterpret_cast<float*>(ws + L.split);
+    g.plane_a = plane_len(M, N);
     if (e == hipSuccess && dx) {
-        LinGemm g{};
-        g.a = dz;
+        g.a = L.direct ? lin_flat(dy, SDM_BF16, M, N, N) : plane_mat(ws + L.dz, M, N, false);
         g.b = lin_flat(w, w_dtype, N, K, K);
-        g.tb = true;
+        if (w_dtype == SDM_F32) {
+            e = sdm_launch_linear_parts(g.b, 3, up64(N), up64(K), ws + L.w, st);
+            g.b = plane_mat(ws + L.w, N, K, true);
+            g.plane_b = plane_len(N, K);
+        }
         g.I = M;
         g.J = K;
         g.R = N;
-        g.ctype = w_dtype;
         g.out = lin_tokens(dx, x_dtype, B, T, K, x_heads);
         g.split = L.px.split;
         g.big = L.px.big;
-        g.part = split;
-        e = sdm_launch_linear(g, st);
+        if (e == hipSuccess) e = sdm_launch_linear(g, st);
     }
     if (e == hipSuccess && dw) {
-        LinGemm g{};
-        g.a = dz;
-        g.b = xm;
-        g.ta = g.tb = true;
+        g.a = L.direct ? lin_flat(dy, SDM_BF16, M, N, N) : plane_mat(ws + L.dz, M, N, true);
+        g.ta = true;
+        g.b = lin_tokens(x, x_dtype, B, T, K, x_heads);
+        if (x_dtype == SDM_F32) {
+            e = sdm_launch_linear_parts(g.b, np, up64(M), up64(K), ws + L.x, st);
+            g.b = plane_mat(ws + L.x, M, K, true);
+            g.plane_b = plane_len(M, K);
+        }
         g.I = N;
         g.J = K;
         g.R = M;
-        g.ctype = w_dtype;
         g.out = lin_flat(dw, w_dtype, N, K, K);
         g.split = L.pw.split;
         g.big = L.pw.big;
-        g.part = split;
-        e = sdm_launch_linear(g, st);
+        if (e == hipSuccess) e = sdm_launch_linear(g, st);
     }
     return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear_bwd launch");
 }

@@ -33,7 +33,7 @@ SIZES = [(dict(B=-1), -1), (dict(T=-1), -1), (dict(K=0), -1), (dict(N=0), -1), (
 @pytest.mark.parametrize("kw,code", SIZES + [
     (dict(y=None), -1), (dict(y=A + 8), -1), (dict(z=A + 4), -1), (dict(res=A + 2), -1), (dict(bias=A + 2), -1),
     (dict(yd=2), -1), (dict(xd=0, wd=0, yd=1), -1), (dict(res=A, yh=8), -1),
-    (dict(B=1, T=1, K=4096, ws=None), -1), (dict(B=1, T=1, K=4096, wsb=16), -3)])
+    (dict(xd=0, wd=0, yd=0, ws=None), -1), (dict(xd=0, wd=0, yd=0, wsb=16), -3)])
 def test_forward_refuses(kw, code):
     assert fwd(**kw) == code
     assert L.sdm_last_error()
