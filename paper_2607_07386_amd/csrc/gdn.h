@@ -221,6 +221,21 @@ GDN_DEV float gdn_ldf(__amdgpu_buffer_rsrc_t r, uint32_t off) {
 GDN_DEV void gdn_stf(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
     __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, (int)off, 0, 0);
 }
+template <typename VT>
+GDN_DEV float gdn_ld1(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    if constexpr (sizeof(VT) == 4) return gdn_ldf(r, off);
+    else return __uint_as_float((uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, (int)off, 0, 0) << 16);
+}
+// eight values of a row from its place p on (zeros past the row's n values)
+GDN_DEV void gdn_ld8(__amdgpu_buffer_rsrc_t r, uint32_t off, int p, int n, float (&x)[8]) {
+    const v4f a = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(p < n ? off : GDN_OUT), 0, 0));
+    const v4f b = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(r, (int)(p + 4 < n ? off + 16 : GDN_OUT), 0, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[i] = a[i];
+        x[4 + i] = b[i];
+    }
+}
 // The fragments (m, 0 .. N-1) of 16 rows of a bf16 matrix of `rows` rows of n values
 // (n % 4 == 0): lane row gdn_row(m, lane & 15).  Rows and depths past the end are zero.
 template <int N>

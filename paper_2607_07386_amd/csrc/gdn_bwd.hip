@@ -313,126 +313,159 @@ hipError_t launch_adjoint_staged(const GdnArgs& a, hipStream_t st) {
 
 // ---------------------------------------------------------------- gradients
 constexpr int LD = 68;
+// bytes of the staged fragments, or of the two 64x64 matrices that take their place
+constexpr size_t grads_stage(int ktn) {
+    const size_t stage = (size_t)(4 * ktn + 4) * 3 * GDN_FRAG * 2, pairs = (size_t)2 * 64 * LD * 4;
+    return stage > pairs ? stage : pairs;
+}
 
 // One workgroup per (key head, chunk), over the heads that share the key head in
-// order (their dq, dk add up in registers, reproducibly).  Wave w holds tokens
-// 16w .. 16w+15.  Per 32 columns of d_v the workgroup stages S0, dS1 and X once
-// as fragments in LDS; a row of a matrix is the same fragment as an A or a B
-// operand, so every product over d_v reads its rows straight from memory.
+// order (their dq, dk add up reproducibly).  Eight waves: wave w holds
+// tokens 16 (w & 3) .. + 15 and one half (w >> 2) of the columns of d_k.  Per 32 columns of
+// d_v the workgroup stages S0, dS1 and X once as fragments in LDS, the next columns'
+// values being fetched meanwhile; a row of a matrix is the same fragment as an A or
+// a B operand, so every product over d_v reads its rows straight from memory.
 template <typename VT, int KTN>
-__global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
-    constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN;
+__global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
+    constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN, DH = KTN;   // DH: a wave's tiles of 16 columns of d_k
+    constexpr int SR = (DT + 7) / 8;                            // tiles of S0, dS1 that a wave stages
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* sS = reinterpret_cast<uint16_t*>(smem);                  // [DT][3] fragments
     uint16_t* sD = sS + DT * 3 * GDN_FRAG;
     uint16_t* sX = sD + DT * 3 * GDN_FRAG;                             // [4][3]
     float* mQ = reinterpret_cast<float*>(smem);                        // after the products, in their place
     float* mB = mQ + 64 * LD;
-    constexpr size_t STAGE = (size_t)(2 * DT + 4) * 3 * GDN_FRAG * 2;
-    constexpr size_t PAIRS = (size_t)2 * 64 * LD * 4;
-    float* mP = reinterpret_cast<float*>(smem + (STAGE > PAIRS ? STAGE : PAIRS));
+    float* mP = reinterpret_cast<float*>(smem + grads_stage(KTN));
     float* mN = mP + 64 * LD;
-    float* vlh = mN + 64 * LD;
-    float *vll = vlh + 64, *vb = vll + 64, *rEnd = vb + 64, *rFrom = rEnd + 64, *rThr = rFrom + 64, *rCol = rThr + 64,
-          *rCross = rCol + 64;
+    float* sV = mN + 64 * LD;                                          // the chunk's vectors
+    const float *vlh = sV + GDN_V_LHI * 64, *vll = sV + GDN_V_LLO * 64, *vb = sV + GDN_V_BETA * 64;
+    float *rEnd = sV + GDN_VEC * 64, *rFrom = rEnd + 128, *rThr = rFrom + 128, *rCol = rThr + 64, *rCross = rCol + 64;
 
     const int c = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, G = a.H / a.Hk;
-    const int len = gdn_len(a, b), t0 = c * GDN_C;
-    if (t0 >= len) return;
-    const int tid = threadIdx.x, lane = lane_id(), w = tid >> 6, r16 = lane & 15, g = lane >> 4;
+    const int len = gdn_len(a, b), t0 = c * GDN_C, left = len - t0;
+    if (left <= 0) return;
+    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15,
+              g = lane >> 4;
+    const int w = wave & 3, half = wave >> 2, d0 = half * DH;
     const size_t tq = (size_t)(b * a.Hk + hk) * a.T + t0;
-    const VT* kp = static_cast<const VT*>(a.k) + tq * a.dk;
-    const VT* qp = static_cast<const VT*>(a.q) + tq * a.dk;
     const size_t ck = (size_t)(b * a.Hk + hk) * a.nC + c;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    const int arow = 16 * w + r16;            // the A operands' token
-    const bool aok = t0 + arow < len;
+    const int arow = gdn_row(w, r16);         // the A operands' token; in the C layout gdn_row(w, 4 g + r)
+    const int wk = w >> 1;                    // the 32 tokens that hold the wave's
     const int dvb = (a.dv + 31) / 32;
+    const uint32_t rows_bytes = (uint32_t)min(left, GDN_C) * a.dv * 4, st_bytes = (uint32_t)a.dk * a.dv * 4;
 
-    sdm_f32x4 dq[DT], dk[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d) dq[d] = dk[d] = zero;
+    const size_t kq_n = (size_t)min(left, GDN_C) * a.dk;
+    const auto bdq = gdn_buf(a.dq + tq * a.dk, kq_n * 4), bdk = gdn_buf(a.dkk + tq * a.dk, kq_n * 4);
 
     for (int hg = 0; hg < G; ++hg) {
         const int bh = b * a.H + hk * G + hg;
         const size_t ch = (size_t)bh * a.nC + c, tv = (size_t)bh * a.T + t0;
         const float* vec = a.vec + ch * GDN_VEC * 64;
-        const float* S0 = a.saved_S + ch * a.dk * a.dv;
-        const float* S1 = a.dS + ch * a.dk * a.dv;
-        const float* xr = a.saved_X + (tv + arow) * a.dv;
-        const float* yr = a.dy + (tv + arow) * a.dv;
-        const float* rr = a.dvv + (tv + arow) * a.dv;
+        // the fragments of k and q are the same for every head; said to change, they are
+        // read after the products and not kept in registers across them
+        const uint16_t *kth = a.kt, *qth = a.qt;
+        asm volatile("" : "+s"(kth), "+s"(qth));
+        const auto bS = gdn_buf(a.saved_S + ch * a.dk * a.dv, st_bytes), bD = gdn_buf(a.dS + ch * a.dk * a.dv, st_bytes);
+        const auto bX = gdn_buf(a.saved_X + tv * a.dv, rows_bytes), bY = gdn_buf(a.dy + tv * a.dv, rows_bytes),
+                   bR = gdn_buf(a.dvv + tv * a.dv, rows_bytes);
+        // this lane's next 8 values of a row of each matrix
+        float xX[8], xY[8], xR[8], xS[SR][8], xD[SR][8];
+        const auto fetch = [&](int kb) {
+            const uint32_t o = (uint32_t)(arow * a.dv + 32 * kb + 8 * g) * 4;
+            const int p = 32 * kb + 8 * g;
+            gdn_ld8(bX, o, p, a.dv, xX);
+            gdn_ld8(bY, o, p, a.dv, xY);
+            gdn_ld8(bR, o, p, a.dv, xR);
+#pragma unroll
+            for (int i = 0; i < SR; ++i) {
+                const int d = wave + 8 * i;
+                const uint32_t os = d < DT ? (uint32_t)(gdn_row(d, r16) * a.dv + 32 * kb + 8 * g) * 4 : GDN_OUT;
+                gdn_ld8(bS, os, p, a.dv, xS[i]);
+                gdn_ld8(bD, os, p, a.dv, xD[i]);
+            }
+        };
+        fetch(0);
         __syncthreads();                      // the previous head's use of LDS
-        if (tid < 64) {
-            vlh[tid] = vec[GDN_V_LHI * 64 + tid];
-            vll[tid] = vec[GDN_V_LLO * 64 + tid];
-            vb[tid] = vec[GDN_V_BETA * 64 + tid];
-        }
-        sdm_f32x4 M1[DT], M2[DT], M3[DT], Z2[4], Z[4];
+        if (tid < GDN_VEC * 64) sV[tid] = vec[tid];
+        sdm_f32x4 M1[DH], M2[DH], M3[DH], Z[4];   // Z: dY X^T in the first half's waves, dR X^T in the second's
 #pragma unroll
-        for (int d = 0; d < DT; ++d) M1[d] = M2[d] = M3[d] = zero;
+        for (int d = 0; d < DH; ++d) M1[d] = M2[d] = M3[d] = zero;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) Z2[j] = Z[j] = zero;
+        for (int j = 0; j < 4; ++j) Z[j] = zero;
         float through = 0.f;
         for (int kb = 0; kb < dvb; ++kb) {
-            const GdnFrag<3> fx = gdn_row_frag<3>(xr, kb, a.dv, aok);
-            const GdnFrag<3> fy = gdn_row_frag<3>(yr, kb, a.dv, aok);
-            const GdnFrag<3> fr = gdn_row_frag<3>(rr, kb, a.dv, aok);
-            gdn_store_frag<3>(sX, w, fx);
-            for (int d = w; d < DT; d += 4) {
-                const int row = gdn_row(d, r16);
-                float x0[8], x1[8];
-                gdn_row8(S0 + (size_t)row * a.dv, kb, a.dv, row < a.dk, x0);
-                gdn_row8(S1 + (size_t)row * a.dv, kb, a.dv, row < a.dk, x1);
+            const GdnFrag<3> fx = gdn_split(xX), fy = gdn_split(xY), fr = gdn_split(xR);
+            if (half == 0) gdn_store_frag<3>(sX, w, fx);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) through = fmaf(x0[i], x1[i], through);
-                gdn_store_frag<3>(sS, d, gdn_split(x0));
-                gdn_store_frag<3>(sD, d, gdn_split(x1));
+            for (int i = 0; i < SR; ++i) {
+                const int d = wave + 8 * i;
+                if (d < DT) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) through = fmaf(xS[i][j], xD[i][j], through);
+                    gdn_store_frag<3>(sS, d, gdn_split(xS[i]));
+                    gdn_store_frag<3>(sD, d, gdn_split(xD[i]));
+                }
             }
+            fetch(min(kb + 1, dvb - 1));
             __syncthreads();
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const GdnFrag<3> s0 = gdn_load_frag<3>(sS, d);
+            for (int d = 0; d < DH; ++d) {
+                const GdnFrag<3> s0 = gdn_load_frag<3>(sS, d0 + d);
                 M2[d] = gdn_mm(fy, s0, M2[d]);
                 M3[d] = gdn_mm(fr, s0, M3[d]);
-                M1[d] = gdn_mm(fx, gdn_load_frag<3>(sD, d), M1[d]);
+                M1[d] = gdn_mm(fx, gdn_load_frag<3>(sD, d0 + d), M1[d]);
+                __builtin_amdgcn_sched_barrier(0);   // one tile's fragments at a time: all of them would spill
             }
+            const GdnFrag<3> fz = half == 0 ? fy : fr;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j > w) break;
-                const GdnFrag<3> x = gdn_load_frag<3>(sX, j);
-                Z2[j] = gdn_mm(fy, x, Z2[j]);
-                Z[j] = gdn_mm(fr, x, Z[j]);
-            }
+            for (int j = 0; j < 4; ++j)
+                if (j >> 1 <= wk) Z[j] = gdn_mm(fz, gdn_load_frag<3>(sX, j), Z[j]);
             __syncthreads();
         }
+        __builtin_amdgcn_sched_barrier(0);
         through = wave_sum(through);
-        if (lane == 0) rThr[w] = through;
-        // rows of M against q and k; dq, dk without the pairs' part
-        float gam[4], en[4], be[4], pe[4], pf[4];
+        if (lane == 0) rThr[wave] = through;
+        // everything the rest reads from memory, in one batch: the fragments of K^T and Q^T
+        // (this wave's own tokens are eight of the depths each lane holds) and P or N
+        GdnFrag<NT> fk[DH][2], fq[DH][2];
+        float pn[4][4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * w + 4 * g + r;
-            gam[r] = vec[GDN_V_GAM * 64 + i];
-            en[r] = vec[GDN_V_END * 64 + i];
-            be[r] = vec[GDN_V_BETA * 64 + i];
-            pe[r] = pf[r] = 0.f;
+        for (int d = 0; d < DH; ++d)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                fk[d][kb] = gdn_load_frag<NT>(kth, (ck * DT + d0 + d) * 2 + kb);
+                fq[d][kb] = gdn_load_frag<NT>(qth, (ck * DT + d0 + d) * 2 + kb);
+            }
+        {
+            const auto bpn = gdn_buf((half == 0 ? a.pm : a.nm) + ch * 64 * 64, 64 * 64 * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    pn[j][r] = gdn_ldf(bpn, (uint32_t)(gdn_row(w, 4 * g + r) * 64 + gdn_row(j, r16)) * 4);
         }
+        // rows of M against q and k; then dq (in M2) and dk (in M1) without the pairs' part
+        const int i0 = gdn_row(w, 4 * g);
+        const v4f gam = ld4(sV + GDN_V_GAM * 64 + i0), en = ld4(sV + GDN_V_END * 64 + i0), be = ld4(vb + i0);
+        float pe[4] = {0.f, 0.f, 0.f, 0.f}, pf[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-            const int dc = gdn_row(d, r16);
+        for (int d = 0; d < DH; ++d)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int i = 16 * w + 4 * g + r;
-                const bool ok = dc < a.dk && t0 + i < len;
-                const float kv = ok ? to_f32(kp[(size_t)i * a.dk + dc]) : 0.f;
-                const float qv = ok ? to_f32(qp[(size_t)i * a.dk + dc]) : 0.f;
+                float kv = 0.f, qv = 0.f;
+#pragma unroll
+                for (int x = NT - 1; x >= 0; --x) {
+                    // which of the two 32-token blocks, and which half of the lane's eight, is the wave's
+                    const sdm_bf16x8 tk = wk ? fk[d][1].t[x] : fk[d][0].t[x], tq8 = wk ? fq[d][1].t[x] : fq[d][0].t[x];
+                    kv += (float)(w & 1 ? tk[4 + r] : tk[r]);
+                    qv += (float)(w & 1 ? tq8[4 + r] : tq8[r]);
+                }
                 pe[r] = fmaf(kv, M1[d][r], pe[r]);
                 pf[r] = fmaf(qv, M2[d][r], fmaf(-kv, M3[d][r], pf[r]));
-                dq[d][r] = fmaf(gam[r], M2[d][r], dq[d][r]);
-                dk[d][r] += be[r] * en[r] * M1[d][r] - gam[r] * M3[d][r];
+                M2[d][r] *= gam[r];
+                M1[d][r] = be[r] * en[r] * M1[d][r] - gam[r] * M3[d][r];
             }
-        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
@@ -441,81 +474,68 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
                 pf[r] += xor_lane_f(pf[r], m);
             }
             if (r16 == 0) {
-                rEnd[16 * w + 4 * g + r] = en[r] * pe[r];
-                rFrom[16 * w + 4 * g + r] = gam[r] * pf[r];
+                rEnd[half * 64 + i0 + r] = en[r] * pe[r];
+                rFrom[half * 64 + i0 + r] = gam[r] * pf[r];
             }
         }
-        // the pairs
+        // the pairs: P . Z2 in mQ, N . Z in mB
+        {
+            float *to = half == 0 ? mP : mN, *to2 = half == 0 ? mQ : mB;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int cj = 16 * j + r16;
+            for (int j = 0; j < 4; ++j) {
+                const int cj = gdn_row(j, r16);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * w + 4 * g + r;
-                float p = 0.f, n = 0.f, q = 0.f;
-                if (cj <= i) {
-                    const float bd = vb[cj] * gdn_decay(vlh[i], vll[i], vlh[cj], vll[cj]);
-                    p = Z2[j][r] * bd;
-                    n = cj < i ? Z[j][r] * bd : 0.f;
-                    q = a.pm[(ch * 64 + i) * 64 + cj] * Z2[j][r];
-                    if (cj < i) q -= a.nm[(ch * 64 + i) * 64 + cj] * Z[j][r];
+                for (int r = 0; r < 4; ++r) {
+                    const int i = i0 + r;
+                    const bool on = cj < i + (half == 0);
+                    const float d = gdn_decay(vlh[i], vll[i], vlh[cj], vll[cj]);   // may overflow above the diagonal
+                    to[i * LD + cj] = on ? Z[j][r] * (vb[cj] * d) : 0.f;
+                    to2[i * LD + cj] = on ? Z[j][r] * pn[j][r] : 0.f;
                 }
-                mP[i * LD + cj] = p;
-                mN[i * LD + cj] = n;
-                mQ[i * LD + cj] = q;
             }
         }
         __syncthreads();
-        {   // mB[i][t] = sum over j < t of mQ[i][j] beta_j: four threads a row, 16 columns each
-            const int i = tid >> 2, s = tid & 3;
-            float part = 0.f;
+        {   // mQ <- P . Z2 - N . Z, mB[i][t] = sum over j < t of mQ[i][j] beta_j: eight threads a row
+            const int i = tid >> 3, s = tid & 7;
+            float q[8], part = 0.f;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) part = fmaf(mQ[i * LD + 16 * s + j], vb[16 * s + j], part);
-            const float p1 = __shfl(part, (lane & ~3) + 0, 64), p2 = __shfl(part, (lane & ~3) + 1, 64),
-                        p3 = __shfl(part, (lane & ~3) + 2, 64);
-            float run = s == 0 ? 0.f : s == 1 ? p1 : s == 2 ? p1 + p2 : p1 + p2 + p3;
+            for (int j = 0; j < 8; ++j) {
+                q[j] = mQ[i * LD + 8 * s + j] - mB[i * LD + 8 * s + j];
+                mQ[i * LD + 8 * s + j] = q[j];
+                part = fmaf(q[j], vb[8 * s + j], part);
+            }
+            float run = part;                 // inclusive over the eight threads, then without this one's
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                mB[i * LD + 16 * s + j] = run;
-                run = fmaf(mQ[i * LD + 16 * s + j], vb[16 * s + j], run);
+            for (int m = 1; m < 8; m <<= 1) {
+                const float o = __shfl_up(run, m, 8);
+                if (s >= m) run += o;
+            }
+            run = __shfl_up(run, 1, 8);
+            if (s == 0) run = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                mB[i * LD + 8 * s + j] = run;
+                run = fmaf(q[j], vb[8 * s + j], run);
             }
         }
         __syncthreads();
         {   // per token: column sums of mQ, and of mB from the token's own row down
-            const int t = tid >> 2, s = tid & 3;
+            const int t = tid >> 3, s = tid & 7;
             float cs = 0.f, cr = 0.f;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int i = 16 * s + j;
+            for (int j = 0; j < 8; ++j) {
+                const int i = s + 8 * j;
                 cs += mQ[i * LD + t];
                 cr += i >= t ? mB[i * LD + t] : 0.f;
             }
-            cs += xor_lane_f(cs, 1);
-            cr += xor_lane_f(cr, 1);
-            cs += xor_lane_f(cs, 2);
-            cr += xor_lane_f(cr, 2);
+#pragma unroll
+            for (int m = 1; m < 8; m <<= 1) {
+                cs += xor_lane_f(cs, m);
+                cr += xor_lane_f(cr, m);
+            }
             if (s == 0) {
                 rCol[t] = cs;
                 rCross[t] = cr;
-            }
-        }
-        __syncthreads();
-        if (w == 0) {
-            const bool ok = t0 + lane < len;
-            const float end = rEnd[lane], be_end = vb[lane] * end;
-            float suf = rFrom[lane], pre = be_end;
-#pragma unroll
-            for (int m = 1; m < 64; m <<= 1) {
-                const float o = __shfl_down(suf, m, 64), u = __shfl_up(pre, m, 64);
-                if (lane + m < 64) suf += o;
-                if (lane >= m) pre += u;
-            }
-            const float before = __shfl_up(pre, 1, 64);
-            const float thr = vec[GDN_V_GAM * 64 + 63] * (rThr[0] + rThr[1] + rThr[2] + rThr[3]);
-            const float dl = rCross[lane] + suf + (lane ? before : 0.f) + thr;
-            if (ok) {
-                a.dalpha[tv + lane] = dl / vec[GDN_V_ALPHA * 64 + lane];
-                a.dbeta[tv + lane] = rCol[lane] + end;
             }
         }
         // dq += mP K;  dk += mP^T Q - (mN + mN^T) K
@@ -531,24 +551,43 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
             }
             const GdnFrag<3> fp = gdn_split(xp), ft = gdn_split(xt), fn = gdn_split(xn);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const GdnFrag<NT> k = gdn_load_frag<NT>(a.kt, (ck * DT + d) * 2 + kb);
-                const GdnFrag<NT> q = gdn_load_frag<NT>(a.qt, (ck * DT + d) * 2 + kb);
-                dq[d] = gdn_mm(fp, k, dq[d]);
-                dk[d] = gdn_mm(ft, q, dk[d]);
-                dk[d] = gdn_mm(fn, k, dk[d]);
+            for (int d = 0; d < DH; ++d) {
+                M2[d] = gdn_mm(fp, fk[d][kb], M2[d]);
+                M1[d] = gdn_mm(ft, fq[d][kb], M1[d]);
+                M1[d] = gdn_mm(fn, fk[d][kb], M1[d]);
             }
         }
-    }
+        // added to what the heads before left there (this thread's own stores)
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-        const int dc = gdn_row(d, r16);
+        for (int d = 0; d < DH; ++d) {
+            const int dc = gdn_row(d0 + d, r16);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int i = 16 * w + 4 * g + r;
-            if (dc < a.dk && t0 + i < len) {
-                a.dq[(tq + i) * a.dk + dc] = dq[d][r];
-                a.dkk[(tq + i) * a.dk + dc] = dk[d][r];
+            for (int r = 0; r < 4; ++r) {
+                const uint32_t o = dc < a.dk ? (uint32_t)((i0 + r) * a.dk + dc) * 4 : GDN_OUT;
+                const float q0 = hg ? gdn_ldf(bdq, o) : 0.f, k0 = hg ? gdn_ldf(bdk, o) : 0.f;
+                gdn_stf(bdq, o, q0 + M2[d][r]);
+                gdn_stf(bdk, o, k0 + M1[d][r]);
+            }
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const bool ok = lane < left;
+            const float end = rEnd[lane] + rEnd[64 + lane], be_end = vb[lane] * end;
+            float suf = rFrom[lane] + rFrom[64 + lane], pre = be_end;
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) {
+                const float o = __shfl_down(suf, m, 64), u = __shfl_up(pre, m, 64);
+                if (lane + m < 64) suf += o;
+                if (lane >= m) pre += u;
+            }
+            const float before = __shfl_up(pre, 1, 64);
+            float thr = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) thr += rThr[i];
+            const float dl = rCross[lane] + suf + (lane ? before : 0.f) + sV[GDN_V_GAM * 64 + 63] * thr;
+            if (ok) {
+                a.dalpha[tv + lane] = dl / sV[GDN_V_ALPHA * 64 + lane];
+                a.dbeta[tv + lane] = rCol[lane] + end;
             }
         }
     }
@@ -556,12 +595,11 @@ __global__ __launch_bounds__(256, 1) void gdn_grads_kernel(GdnArgs a) {
 
 template <typename VT, int KTN>
 hipError_t launch_grads(const GdnArgs& a, hipStream_t st) {
-    constexpr size_t stage = (size_t)(4 * KTN + 4) * 3 * GDN_FRAG * 2, pairs = (size_t)2 * 64 * LD * 4;
-    constexpr size_t lds = (stage > pairs ? stage : pairs) + pairs + 8 * 64 * 4;
+    constexpr size_t lds = grads_stage(KTN) + (size_t)2 * 64 * LD * 4 + (GDN_VEC + 7) * 64 * 4;
     const auto kfn = gdn_grads_kernel<VT, KTN>;
     hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    kfn<<<dim3(a.nC, a.B * a.Hk), 256, lds, st>>>(a);
+    kfn<<<dim3(a.nC, a.B * a.Hk), 512, lds, st>>>(a);
     return hipGetLastError();
 }
 
