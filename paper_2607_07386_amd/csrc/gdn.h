@@ -236,50 +236,80 @@ GDN_DEV void gdn_ld8(__amdgpu_buffer_rsrc_t r, uint32_t off, int p, int n, float
         x[4 + i] = b[i];
     }
 }
-// The fragments (m, 0 .. N-1) of 16 rows of a bf16 matrix of `rows` rows of n values
-// (n % 4 == 0): lane row gdn_row(m, lane & 15).  Rows and depths past the end are zero.
-template <int N>
-GDN_DEV void gdn_fetch_rows(u4v (&r)[N], const bf16_t* base, int m, int rows, int n) {
+// Fragments first .. first + N - 1 of the [4][KTN] of 64 rows of a bf16 matrix of `rows` rows of
+// n values (n % 4 == 0): fragment (m, kb), lane row gdn_row(m, lane & 15).  Rows and depths past
+// the end are zero.
+template <int KTN, int N>
+GDN_DEV void gdn_fetch_rows(u4v (&r)[N], const bf16_t* base, int first, int rows, int n) {
     const auto buf = gdn_buf(base, (size_t)min(rows, GDN_C) * n * 2);
-    const uint32_t row = gdn_row(m, lane_id() & 15) * n * 2;
-    const int p0 = 8 * (lane_id() >> 4);
-    if (n % 8 == 0) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int p = 32 * i + p0;
-            r[i] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(buf, (int)(p < n ? row + p * 2 : GDN_OUT), 0, 0));
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int p = 32 * i + p0;
-            const u2v lo = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p < n ? row + p * 2 : GDN_OUT), 0, 0));
-            const u2v hi = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p + 4 < n ? row + p * 2 + 8 : GDN_OUT), 0, 0));
+    for (int i = 0; i < N; ++i) {
+        const int m = (first + i) / KTN, p = 32 * ((first + i) % KTN) + 8 * (lane_id() >> 4);
+        const uint32_t o = (uint32_t)(gdn_row(m, lane_id() & 15) * n + p) * 2;
+        if (n % 8 == 0) {
+            r[i] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(buf, (int)(p < n ? o : GDN_OUT), 0, 0));
+        } else {
+            const u2v lo = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p < n ? o : GDN_OUT), 0, 0));
+            const u2v hi = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p + 4 < n ? o + 8 : GDN_OUT), 0, 0));
             r[i] = u4v{lo.x, lo.y, hi.x, hi.y};
         }
     }
 }
-// A state's 16 columns of this lane's column offset `co` (bytes) in the C layout.
-template <int DT>
-GDN_DEV void gdn_load_state(sdm_f32x4 (&S)[DT], const float* p, int dk, int dv, uint32_t co) {
+// Tiles d0 .. d0 + N - 1 of a state's 16 columns at the lane's column offset `co` (bytes), in the C layout.
+template <int N>
+GDN_DEV void gdn_load_state(sdm_f32x4 (&S)[N], const float* p, int d0, int dk, int dv, uint32_t co) {
     const auto buf = gdn_buf(p, p ? (size_t)dk * dv * 4 : 0);
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int d = 0; d < N; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[d][r] = gdn_ldf(buf, gdn_row(d, 4 * (lane_id() >> 4) + r) * dv * 4 + co);
+        for (int r = 0; r < 4; ++r) S[d][r] = gdn_ldf(buf, gdn_row(d0 + d, 4 * (lane_id() >> 4) + r) * dv * 4 + co);
 }
-template <int DT>
-GDN_DEV void gdn_store_state(const sdm_f32x4 (&S)[DT], float* p, int dk, int dv, uint32_t co) {
+template <int N>
+GDN_DEV void gdn_store_state(const sdm_f32x4 (&S)[N], float* p, int d0, int dk, int dv, uint32_t co) {
     const auto buf = gdn_buf(p, (size_t)dk * dv * 4);
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int d = 0; d < N; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) gdn_stf(buf, gdn_row(d, 4 * (lane_id() >> 4) + r) * dv * 4 + co, S[d][r]);
+        for (int r = 0; r < 4; ++r) gdn_stf(buf, gdn_row(d0 + d, 4 * (lane_id() >> 4) + r) * dv * 4 + co, S[d][r]);
 }
 template <int N>
 GDN_DEV void gdn_stage(uint16_t* lds, int first, const u4v (&r)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) *reinterpret_cast<u4v*>(lds + (first + i) * GDN_FRAG + lane_id() * 8) = r[i];
+}
+
+// Fragments `wave`, `wave` + NW, ... of the n laid out at base (past the end: the last one again).
+template <int NW, int N>
+GDN_DEV void gdn_fetch_turns(u4v (&r)[N], const uint16_t* base, int n, int wave) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        r[i] = *reinterpret_cast<const u4v*>(base + (size_t)min(wave + NW * i, n - 1) * GDN_FRAG + lane_id() * 8);
+}
+template <int NW, int N>
+GDN_DEV void gdn_stage_turns(uint16_t* lds, int n, int wave, const u4v (&r)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        *reinterpret_cast<u4v*>(lds + min(wave + NW * i, n - 1) * GDN_FRAG + lane_id() * 8) = r[i];
+}
+// Rows gdn_row(dt, .) of the transpose of a matrix that stands in LDS as the fragments
+// [4][KTN] of its 64 rows, depths 32 kb .. 32 kb + 31 (its rows): the transposing read takes
+// four rows of four columns from four lanes each, wherever they are.
+template <int KTN>
+GDN_DEV GdnFrag<1> gdn_turned_frag(const uint16_t* lds, int dt, int kb) {
+    typedef short s4 __attribute__((ext_vector_type(4)));
+    const int l = lane_id(), row = 4 * (l >> 4) + ((l & 15) >> 2);   // row of the source tile
+    union {
+        s4 s[2];
+        sdm_bf16x8 v;
+    } f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint16_t* p = lds + ((2 * kb + h) * KTN + (dt >> 1)) * GDN_FRAG + ((l & 3) * 16 + row) * 8 + (dt & 1) * 4;
+        f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p);
+    }
+    GdnFrag<1> r;
+    r.t[0] = f.v;
+    return r;
 }
 
 // exp(lambda_i - lambda_j), the sums of log alpha held as two floats each (a

@@ -277,46 +277,33 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
         }
         gdn_store_frag<3>(f < GDN_BLKS ? a.tf : a.pf, ch * GDN_BLKS + blk, gdn_split(x));
     }
-    // K^T (and Q^T) of the key head: rows of d_k, depth = tokens
-    if (h % G == 0) {
+    // fp32: K^T (and Q^T) of the key head, rows of d_k, depth = tokens (bf16 scans turn K in LDS)
+    if constexpr (NT == 3) {
+        if (h % G) return;
         const size_t ck = (size_t)(b * a.Hk + hk) * a.nC + c;
         for (int f = w; f < (BWD ? 2 : 1) * DT * 2; f += 4) {
             const int id = f % (DT * 2), dt = id >> 1, kb = id & 1;
             const VT* src = f < DT * 2 ? kp : qp;
             const int d = gdn_row(dt, r16);
-            GdnFrag<NT> fr;
-            if constexpr (NT == 1) {
-                union {
-                    uint16_t u[8];
-                    sdm_bf16x8 v;
-                } x;
+            float x[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = 32 * kb + 8 * g + i;
-                    x.u[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d].bits : (uint16_t)0;
-                }
-                fr.t[0] = x.v;
-            } else {
-                float x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int t = 32 * kb + 8 * g + i;
-                    x[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d] : 0.f;
-                }
-                fr = gdn_split(x);
+            for (int i = 0; i < 8; ++i) {
+                const int t = 32 * kb + 8 * g + i;
+                x[i] = d < a.dk && t0 + t < len ? src[(size_t)t * a.dk + d] : 0.f;
             }
-            gdn_store_frag<NT>(f < DT * 2 ? a.kt : a.qt, ck * DT * 2 + id, fr);
+            gdn_store_frag<3>(f < DT * 2 ? a.kt : a.qt, ck * DT * 2 + id, gdn_split(x));
         }
     }
 }
 
 // ---------------------------------------------------------------- scan
-// One wave per 16 columns of a stream's state, four to a workgroup; the waves
+// fp32 inputs: one wave per 16 columns of a stream's state, four to a workgroup; the waves
 // share nothing (each reads the chunk's fragments itself) and never wait for
 // one another.  The state stays in the C layout of its own update.
-template <typename VT, int KTN, bool SAVE>
+template <int KTN, bool SAVE>
 __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
-    constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN;
+    using VT = float;
+    constexpr int NT = 3, DT = 2 * KTN;
     const int groups = (a.dv + 63) / 64;
     int grp, bh;
     scan_wg_coords<true>(groups, grp, bh);
@@ -439,88 +426,107 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
         }
 }
 
-// The same walk for bf16 inputs with the chunk's fragments staged in LDS, one copy
-// for the workgroup's four waves, each piece fetched into registers a chunk ahead
-// and written over the last one as soon as every wave is done with it.
+// The same walk for bf16 inputs, two waves to 16 columns: half h holds tokens 32 h .. + 31 of the
+// chunk and one half of the state's rows, so that a chunk's chain of dependent products
+// is half as long and twice as many waves share the device.  What a half needs of the
+// other (the state's fragments, R and E of the first 32 tokens, E for the update)
+// passes through LDS.  The chunk's K, Q, T' and P are fetched into registers a chunk
+// ahead and staged once for the workgroup; K^T is K read with the transposing loads.
 template <int KTN>
-constexpr size_t scan_lds() {
-    return (size_t)(12 * KTN + 36) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
-}
+struct ScanCfg {
+    static constexpr int NCT = KTN == 8 ? 2 : 4;       // column tiles of a workgroup
+    static constexpr int NW = 2 * NCT;
+    static constexpr bool QD = KTN == 8;               // Q straight from memory: LDS is full
+    static constexpr int FPW = 4 * KTN / NW;           // fragments of K (and Q) that a wave moves
+    static constexpr int TPW = (18 + NW - 1) / NW;     // of T' (and P)
+    static constexpr int XCH = (KTN + 3) * 3;          // exchanged fragments per column tile: S, then E_a, E'_a, E'_b (R_a)
+    static constexpr size_t LDS =
+        (size_t)(4 * KTN * (QD ? 1 : 2) + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+};
 
 template <int KTN, bool SAVE>
-__global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
-    constexpr int DT = 2 * KTN;
+__global__ __launch_bounds__(ScanCfg<KTN>::NW * 64) void gdn_scan_halves_kernel(GdnArgs a) {
+    using C = ScanCfg<KTN>;
+    constexpr int NW = C::NW, KH = KTN / 2;            // KH: 32-row blocks of the state per wave
     extern __shared__ __align__(16) unsigned char smem[];
-    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // K [4][KTN], then Q
-    uint16_t* sQ = sK + 4 * KTN * GDN_FRAG;
-    uint16_t* sT = sQ + 4 * KTN * GDN_FRAG;                 // T' [6][3], then P
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN]
+    uint16_t* sT = sK + 4 * KTN * GDN_FRAG;                 // T' [6][3]
     uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;
-    uint16_t* sKT = sP + GDN_BLKS * 3 * GDN_FRAG;           // K^T [DT][2]
-    float* sV = reinterpret_cast<float*>(sKT + 4 * KTN * GDN_FRAG);   // [2][gamma, end, beta][64]
+    uint16_t* sX = sP + GDN_BLKS * 3 * GDN_FRAG;            // exchange, per column tile
+    float* sV = reinterpret_cast<float*>(sX + C::NCT * C::XCH * GDN_FRAG);   // [2][gamma, end, beta][64]
+    uint16_t* sQ = reinterpret_cast<uint16_t*>(sV + 2 * 3 * 64);             // [4][KTN] unless QD
 
-    const int groups = (a.dv + 63) / 64;
+    const int groups = (a.dv + 16 * C::NCT - 1) / (16 * C::NCT);
     int grp, bh;
     scan_wg_coords<true>(groups, grp, bh);
     const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
     const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), r16 = lane & 15, g = lane >> 4;
-    const int col = (grp * 4 + w) * 16 + r16;
+    const int ct = w % C::NCT, h = w / C::NCT;
+    const int col = (grp * C::NCT + ct) * 16 + r16;
     const bool cv = col < a.dv;
     const uint32_t co = cv ? col * 4 : GDN_OUT, co2 = cv ? col * 2 : GDN_OUT;   // column offsets: fp32, bf16
     const size_t sn = (size_t)a.dk * a.dv;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    uint16_t* xS = sX + ct * C::XCH * GDN_FRAG;             // [KTN][3]
+    uint16_t *xE = xS + KTN * 3 * GDN_FRAG, *xA = xE + 3 * GDN_FRAG, *xB = xA + 3 * GDN_FRAG;   // xB: R_a until E'_b
 
-    sdm_f32x4 S[DT];
-    gdn_load_state(S, a.state0 ? a.state0 + bh * sn : nullptr, a.dk, a.dv, co);
     const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
     const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
     const bf16_t* vp = static_cast<const bf16_t*>(a.v) + (size_t)bh * a.T * a.dv;
-    const size_t ch0 = (size_t)bh * a.nC, ck0 = (size_t)(b * a.Hk + hk) * a.nC;
+    const size_t ch0 = (size_t)bh * a.nC;
 
-    u4v rK[KTN], rQ[KTN], rT[9], rKT[KTN];
-    float rV, V[4][4];
-    const auto fetch_kq = [&](int c) {
-        const int t0 = c * GDN_C;
-        gdn_fetch_rows(rK, kp + (size_t)t0 * a.dk, w, len - t0, a.dk);
-        gdn_fetch_rows(rQ, qp + (size_t)t0 * a.dk, w, len - t0, a.dk);
-        const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // wave 3 repeats wave 2
+    sdm_f32x4 S[KTN];                                       // this half's tiles
+    GdnFrag<3> sf[KH];                                      // and their fragments
+    gdn_load_state(S, a.state0 ? a.state0 + bh * sn : nullptr, h * KTN, a.dk, a.dv, co);
+    const auto give_state = [&]() {
+#pragma unroll
+        for (int i = 0; i < KH; ++i) {
+            sf[i] = gdn_stack(S[2 * i], S[2 * i + 1]);
+            gdn_store_frag<3>(xS, h * KH + i, sf[i]);
+        }
+    };
+
+    u4v rK[C::FPW], rQ[C::FPW], rT[C::TPW], rP[C::TPW];
+    float rV, V[2][4];
+    const auto fetch_k = [&](int c) { gdn_fetch_rows<KTN>(rK, kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk); };
+    const auto fetch_q = [&](int c) {
+        if constexpr (!C::QD) gdn_fetch_rows<KTN>(rQ, qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // waves 3 on repeat wave 2
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
     };
     const auto fetch_v = [&](int c) {
         const int t0 = c * GDN_C;
         const auto buf = gdn_buf(vp + (size_t)t0 * a.dv, (size_t)min(len - t0, GDN_C) * a.dv * 2);
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                V[m][r] = __uint_as_float((uint32_t)__builtin_amdgcn_raw_buffer_load_b16(
-                                              buf, (int)(gdn_row(m, 4 * g + r) * a.dv * 2 + co2), 0, 0) << 16);
+            for (int r = 0; r < 4; ++r) V[m][r] = gdn_ld1<bf16_t>(buf, gdn_row(2 * h + m, 4 * g + r) * a.dv * 2 + co2);
     };
-    const auto fetch_t = [&](int c) {   // 18 fragments of T' (waves 0, 1), 18 of P
-        const uint16_t* src = w < 2 ? a.tf : a.pf;
-        gdn_fetch(rT, src + (ch0 + c) * GDN_BLKS * 3 * GDN_FRAG, (w & 1) * 9);
-    };
-    const auto fetch_kt = [&](int c) { gdn_fetch(rKT, a.kt + (ck0 + c) * DT * 2 * GDN_FRAG, w * KTN); };
-    const auto stage_kq = [&](int par) {
-        gdn_stage(sK, w * KTN, rK);
-        gdn_stage(sQ, w * KTN, rQ);
+    const auto fetch_t = [&](int c) { gdn_fetch_turns<NW>(rT, a.tf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
+    const auto fetch_p = [&](int c) { gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
+    const auto stage_k = [&]() { gdn_stage(sK, w * C::FPW, rK); };
+    const auto stage_q = [&](int par) {
+        if constexpr (!C::QD) gdn_stage(sQ, w * C::FPW, rQ);
         if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
     };
-    const auto stage_t = [&]() { gdn_stage(sT, w * 9, rT); };
-    const auto stage_kt = [&]() { gdn_stage(sKT, w * KTN, rKT); };
 
     if (nc > 0) {
-        fetch_kq(0);
+        fetch_k(0);
+        fetch_q(0);
         fetch_v(0);
         fetch_t(0);
-        fetch_kt(0);
-        stage_kq(0);
-        stage_t();
-        stage_kt();
+        fetch_p(0);
+        give_state();
+        stage_k();
+        stage_q(0);
+        gdn_stage_turns<NW>(sT, 18, w, rT);
+        gdn_stage_turns<NW>(sP, 18, w, rP);
         const int c1 = min(1, nc - 1);
-        fetch_kq(c1);
+        fetch_q(c1);
         fetch_t(c1);
-        fetch_kt(c1);
+        fetch_p(c1);
+        fetch_k(c1);
         __syncthreads();
     }
     // (the last chunks fetch and stage once more what nobody reads: without the
@@ -528,92 +534,116 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_staged_kernel(GdnArgs a) {
     for (int c = 0; c < nc; ++c) {
         const int t0 = c * GDN_C, left = len - t0, next = min(c + 2, nc - 1);
         const float* vec = sV + (c & 1) * 3 * 64;
-        const auto ybuf = gdn_buf(a.y + ((size_t)bh * a.T + t0) * a.dv, (size_t)min(left, GDN_C) * a.dv * 4);
-        const auto xbuf = gdn_buf(SAVE ? a.saved_X + ((size_t)bh * a.T + t0) * a.dv : nullptr,
-                                  (size_t)min(left, GDN_C) * a.dv * 4);
-        if constexpr (SAVE) gdn_store_state(S, a.saved_S + (ch0 + c) * sn, a.dk, a.dv, co);
-        sdm_f32x4 R[4], Y[4], X[4];
+        const size_t row0 = (size_t)bh * a.T + t0, rows = min(left, GDN_C);
+        const auto ybuf = gdn_buf(a.y + row0 * a.dv, rows * a.dv * 4);
+        const auto xbuf = gdn_buf(SAVE ? a.saved_X + row0 * a.dv : nullptr, rows * a.dv * 4);
+        if constexpr (SAVE) gdn_store_state(S, a.saved_S + (ch0 + c) * sn, h * KTN, a.dk, a.dv, co);
+        // R = V - gamma K S0 and Y = gamma Q S0 of this half's tokens
+        sdm_f32x4 R[2], Y[2], X[2];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) R[m] = Y[m] = X[m] = zero;
+        for (int m = 0; m < 2; ++m) R[m] = Y[m] = X[m] = zero;
+        const auto rows_by_state = [&](int kb, const GdnFrag<3>& s) {
 #pragma unroll
-        for (int kb = 0; kb < KTN; ++kb) {
-            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
+            for (int m = 0; m < 2; ++m) R[m] = gdn_mm(gdn_load_frag<1>(sK, (2 * h + m) * KTN + kb), s, R[m]);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) R[m] = gdn_mm(gdn_load_frag<1>(sK, m * KTN + kb), s, R[m]);
+            for (int m = 0; m < 2; ++m) {
+                if constexpr (C::QD) {
+                    const int row = gdn_row(2 * h + m, r16);
+                    Y[m] = gdn_mm(gdn_row_frag<1>(qp + (size_t)(t0 + row) * a.dk, kb, a.dk, row < left), s, Y[m]);
+                } else {
+                    Y[m] = gdn_mm(gdn_load_frag<1>(sQ, (2 * h + m) * KTN + kb), s, Y[m]);
+                }
+            }
+        };
 #pragma unroll
-            for (int m = 0; m < 4; ++m) Y[m] = gdn_mm(gdn_load_frag<1>(sQ, m * KTN + kb), s, Y[m]);
-        }
+        for (int i = 0; i < KH; ++i) rows_by_state(h * KH + i, sf[i]);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f gam = ld4(vec + gdn_row(m, 4 * g));
+        for (int i = 0; i < KH; ++i) rows_by_state((1 - h) * KH + i, gdn_load_frag<3>(xS, (1 - h) * KH + i));
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const v4f gam = ld4(vec + gdn_row(2 * h + m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 R[m][r] = fmaf(-gam[r], R[m][r], V[m][r]);   // 0 past the end: K and V are
                 Y[m][r] *= gam[r];
             }
         }
+        const GdnFrag<3> rf = gdn_stack(R[0], R[1]);
+        if (h == 0) gdn_store_frag<3>(xB, 0, rf);
         __syncthreads();
-        stage_kq((c + 1) & 1);
+        stage_q((c + 1) & 1);
         fetch_v(min(c + 1, nc - 1));
-        fetch_kq(next);
+        fetch_q(next);
+        // X = T' R, E = beta X
+        if (h == 1) {
+            const GdnFrag<3> ra = gdn_load_frag<3>(xB, 0);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(R[2 * kb], R[2 * kb + 1]);
-#pragma unroll
-            for (int m = 2 * kb; m < 4; ++m) X[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_low_blk(m, kb)), f, X[m]);
+            for (int m = 0; m < 2; ++m) X[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_low_blk(2 + m, 0)), ra, X[m]);
         }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f be = ld4(vec + 128 + gdn_row(m, 4 * g));
+        for (int m = 0; m < 2; ++m) X[m] = gdn_mm(gdn_load_frag<3>(sT, h ? 3 + 2 * m : m), rf, X[m]);
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const v4f be = ld4(vec + 128 + gdn_row(2 * h + m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                if constexpr (SAVE) gdn_stf(xbuf, t * a.dv * 4 + co, X[m][r]);
+                if constexpr (SAVE) gdn_stf(xbuf, gdn_row(2 * h + m, 4 * g + r) * a.dv * 4 + co, X[m][r]);
                 X[m][r] *= be[r];
             }
         }
+        const GdnFrag<3> ef = gdn_stack(X[0], X[1]);
+        if (h == 0) gdn_store_frag<3>(xE, 0, ef);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
+        for (int m = 0; m < 2; ++m) {
+            const v4f en = ld4(vec + 64 + gdn_row(2 * h + m, 4 * g));
 #pragma unroll
-            for (int m = 2 * kb; m < 4; ++m) Y[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_low_blk(m, kb)), f, Y[m]);
+            for (int r = 0; r < 4; ++r) X[m][r] *= en[r];
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f en = ld4(vec + 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                gdn_stf(ybuf, t * a.dv * 4 + co, Y[m][r]);
-                X[m][r] *= en[r];
-            }
-        }
+        const GdnFrag<3> uf = gdn_stack(X[0], X[1]);
+        gdn_store_frag<3>(h ? xB : xA, 0, uf);
         const float last = vec[63];
         __syncthreads();
-        stage_t();
+        gdn_stage_turns<NW>(sT, 18, w, rT);
         fetch_t(next);
+        // S = gamma S + K^T (C E), then Y += P E
+        {
+            const GdnFrag<3> uo = gdn_load_frag<3>(h ? xA : xB, 0);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) S[d] *= last;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) S[d] = gdn_mm(gdn_load_frag<1>(sKT, d * 2 + kb), f, S[d]);
+            for (int d = 0; d < KTN; ++d) {
+                S[d] *= last;
+                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, h), uf, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, 1 - h), uo, S[d]);
+            }
         }
+        if (h == 1) {
+            const GdnFrag<3> ea = gdn_load_frag<3>(xE, 0);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) Y[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_low_blk(2 + m, 0)), ea, Y[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) Y[m] = gdn_mm(gdn_load_frag<3>(sP, h ? 3 + 2 * m : m), ef, Y[m]);
+        give_state();
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) gdn_stf(ybuf, gdn_row(2 * h + m, 4 * g + r) * a.dv * 4 + co, Y[m][r]);
         __syncthreads();
-        stage_kt();
-        fetch_kt(next);
+        gdn_stage_turns<NW>(sP, 18, w, rP);
+        stage_k();
+        fetch_p(next);
+        fetch_k(next);
+        __syncthreads();
     }
-    gdn_store_state(S, a.stateT + bh * sn, a.dk, a.dv, co);
+    gdn_store_state(S, a.stateT + bh * sn, h * KTN, a.dk, a.dv, co);
 }
 
 template <int KTN, bool SAVE>
-hipError_t launch_scan_staged(const GdnArgs& a, hipStream_t st) {
-    const auto kfn = gdn_scan_staged_kernel<KTN, SAVE>;
-    constexpr size_t lds = scan_lds<KTN>();
-    hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+hipError_t launch_scan_halves(const GdnArgs& a, hipStream_t st) {
+    using C = ScanCfg<KTN>;
+    const auto kfn = gdn_scan_halves_kernel<KTN, SAVE>;
+    hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
     if (e != hipSuccess) return e;
-    kfn<<<dim3((a.dv + 63) / 64 * a.B * a.H), 256, lds, st>>>(a);
+    kfn<<<dim3((a.dv + 16 * C::NCT - 1) / (16 * C::NCT) * a.B * a.H), C::NW * 64, C::LDS, st>>>(a);
     return hipGetLastError();
 }
 
@@ -623,7 +653,8 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
     GdnWs w{};
     const size_t nC = ((size_t)T + GDN_C - 1) / GDN_C;
     const size_t n = (size_t)B * H * nC, nk = (size_t)B * Hk * nC;
-    const size_t dt = (dk <= 32 ? 2 : dk <= 64 ? 4 : dk <= 128 ? 8 : 16), nt = in_dtype == SDM_DT_F32 ? 3 : 1;
+    const size_t dt = dk <= 64 ? 4 : dk <= 128 ? 8 : 16;
+    const bool f32 = in_dtype == SDM_DT_F32;
     size_t o = 0;
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -633,9 +664,9 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
     w.vec = take(n * GDN_VEC * 64 * 4);
     w.tf = take(n * GDN_BLKS * 3 * GDN_FRAG * 2);
     w.pf = take(n * GDN_BLKS * 3 * GDN_FRAG * 2);
-    w.kt = take(nk * dt * 2 * nt * GDN_FRAG * 2);
+    w.kt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
     if (backward) {
-        w.qt = take(nk * dt * 2 * nt * GDN_FRAG * 2);
+        w.qt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
         w.pm = take(n * 64 * 64 * 4);
         w.nm = take(n * 64 * 64 * 4);
         w.dS = take(n * dk * dv * 4);
@@ -646,8 +677,7 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
 
 #define GDN_PICK_KTN(K)                                  \
     do {                                                 \
-        if (a.dk <= 32) K(1);                            \
-        else if (a.dk <= 64) K(2);                       \
+        if (a.dk <= 64) K(2);                            \
         else if (a.dk <= 128) K(4);                      \
         else K(8);                                       \
     } while (0)
@@ -685,10 +715,10 @@ hipError_t sdm_launch_gdn_scan(const GdnArgs& a, hipStream_t st) {
     const bool bf = a.in_dtype == SDM_DT_BF16, save = a.saved_S != nullptr;
 #define K(N)                                                                                 \
     do {                                                                                     \
-        if (bf && save) return launch_scan_staged<N, true>(a, st);                           \
-        else if (bf) return launch_scan_staged<N, false>(a, st);                             \
-        else if (save) gdn_scan_kernel<float, N, true><<<grid, 256, 0, st>>>(a);             \
-        else gdn_scan_kernel<float, N, false><<<grid, 256, 0, st>>>(a);                      \
+        if (bf && save) return launch_scan_halves<N, true>(a, st);                           \
+        else if (bf) return launch_scan_halves<N, false>(a, st);                             \
+        else if (save) gdn_scan_kernel<N, true><<<grid, 256, 0, st>>>(a);             \
+        else gdn_scan_kernel<N, false><<<grid, 256, 0, st>>>(a);                      \
     } while (0)
     GDN_PICK_KTN(K);
 #undef K

@@ -22,9 +22,11 @@
 
 namespace {
 
-template <typename VT, int KTN>
+// fp32 inputs: one wave per 16 columns, as gdn_scan_kernel
+template <int KTN>
 __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
-    constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN;
+    using VT = float;
+    constexpr int NT = 3, DT = 2 * KTN;
     const int groups = (a.dv + 63) / 64;
     int grp, bh;
     scan_wg_coords<true>(groups, grp, bh);
@@ -144,178 +146,222 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
     }
 }
 
-// The same walk for bf16 inputs, fragments staged in LDS as in the forward scan.
+// The same walk for bf16 inputs, two waves to 16 columns as in the forward scan: half h
+// holds tokens 32 h .. + 31 and one half of the state's rows.  dY is read whole by both
+// (its part below needs no exchange); F = diag(beta) dE of the last 32 tokens and -G dR
+// pass through LDS.
 template <int KTN>
-__global__ __launch_bounds__(256, 1) void gdn_adjoint_staged_kernel(GdnArgs a) {
-    constexpr int DT = 2 * KTN;
-    extern __shared__ __align__(16) unsigned char smem[];
-    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // K [4][KTN]
-    uint16_t* sT = sK + 4 * KTN * GDN_FRAG;                 // T'^T [6][3], then P^T
-    uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;
-    uint16_t* sKT = sP + GDN_BLKS * 3 * GDN_FRAG;           // K^T [DT][2], then Q^T
-    uint16_t* sQT = sKT + 4 * KTN * GDN_FRAG;
-    float* sV = reinterpret_cast<float*>(sQT + 4 * KTN * GDN_FRAG);   // [2][gamma, end, beta][64]
+struct AdjCfg {
+    static constexpr int NCT = KTN == 8 ? 1 : 4;
+    static constexpr int NW = 2 * NCT;
+    static constexpr int FPW = 4 * KTN / NW;
+    static constexpr int TPW = (18 + NW - 1) / NW;
+    static constexpr int XCH = (KTN + 3) * 3;          // S, then F_b, N_a, N_b
+    static constexpr size_t LDS = (size_t)(8 * KTN + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+};
 
-    const int groups = (a.dv + 63) / 64;
+template <int KTN>
+__global__ __launch_bounds__(AdjCfg<KTN>::NW * 64) void gdn_adjoint_halves_kernel(GdnArgs a) {
+    using C = AdjCfg<KTN>;
+    constexpr int NW = C::NW, KH = KTN / 2;
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN]
+    uint16_t* sQ = sK + 4 * KTN * GDN_FRAG;
+    uint16_t* sT = sQ + 4 * KTN * GDN_FRAG;                 // T'^T [6][3]
+    uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;            // P^T
+    uint16_t* sX = sP + GDN_BLKS * 3 * GDN_FRAG;
+    float* sV = reinterpret_cast<float*>(sX + C::NCT * C::XCH * GDN_FRAG);   // [2][gamma, end, beta][64]
+
+    const int groups = (a.dv + 16 * C::NCT - 1) / (16 * C::NCT);
     int grp, bh;
     scan_wg_coords<true>(groups, grp, bh);
     const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
     const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id(), r16 = lane & 15, g = lane >> 4;
-    const int col = (grp * 4 + w) * 16 + r16;
-    const bool cv = col < a.dv;
-    const uint32_t co = cv ? col * 4 : GDN_OUT;
+    const int ct = w % C::NCT, h = w / C::NCT;
+    const int col = (grp * C::NCT + ct) * 16 + r16;
+    const uint32_t co = col < a.dv ? col * 4 : GDN_OUT;
     const size_t sn = (size_t)a.dk * a.dv;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+    uint16_t* xS = sX + ct * C::XCH * GDN_FRAG;             // [KTN][3]
+    uint16_t *xF = xS + KTN * 3 * GDN_FRAG, *xA = xF + 3 * GDN_FRAG, *xB = xA + 3 * GDN_FRAG;
 
-    sdm_f32x4 S[DT];
-    gdn_load_state(S, a.dstateT ? a.dstateT + bh * sn : nullptr, a.dk, a.dv, co);
     const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
-    const float* yp = a.dy + (size_t)bh * a.T * a.dv;
-    float* dvp = a.dvv + (size_t)bh * a.T * a.dv;
-    const size_t ch0 = (size_t)bh * a.nC, ck0 = (size_t)(b * a.Hk + hk) * a.nC;
+    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const size_t ch0 = (size_t)bh * a.nC;
 
-    u4v rK[KTN], rT[9], rKT[KTN], rQT[KTN];
+    sdm_f32x4 S[KTN];
+    GdnFrag<3> sf[KH];
+    gdn_load_state(S, a.dstateT ? a.dstateT + bh * sn : nullptr, h * KTN, a.dk, a.dv, co);
+    const auto give_state = [&]() {
+#pragma unroll
+        for (int i = 0; i < KH; ++i) {
+            sf[i] = gdn_stack(S[2 * i], S[2 * i + 1]);
+            gdn_store_frag<3>(xS, h * KH + i, sf[i]);
+        }
+    };
+
+    u4v rK[C::FPW], rQ[C::FPW], rT[C::TPW], rP[C::TPW];
     float rV, rY[4][4];
-    const auto fetch_k = [&](int c) {
-        gdn_fetch_rows(rK, kp + (size_t)c * GDN_C * a.dk, w, len - c * GDN_C, a.dk);
-        const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // wave 3 repeats wave 2
+    const auto fetch_kq = [&](int c) {
+        gdn_fetch_rows<KTN>(rK, kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        gdn_fetch_rows<KTN>(rQ, qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // other waves repeat beta
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
     };
+    float rB = 0.f;                                         // beta where the workgroup has two waves only
     const auto fetch_y = [&](int c) {
-        const auto buf = gdn_buf(yp + (size_t)c * GDN_C * a.dv, (size_t)min(len - c * GDN_C, GDN_C) * a.dv * 4);
+        const auto buf = gdn_buf(a.dy + ((size_t)bh * a.T + (size_t)c * GDN_C) * a.dv, (size_t)min(len - c * GDN_C, GDN_C) * a.dv * 4);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) rY[m][r] = gdn_ldf(buf, gdn_row(m, 4 * g + r) * a.dv * 4 + co);
+        if constexpr (NW == 2) rB = a.vec[(ch0 + c) * GDN_VEC * 64 + GDN_V_BETA * 64 + lane];
     };
-    const auto fetch_t = [&](int c) {
-        const uint16_t* src = w < 2 ? a.tf : a.pf;
-        gdn_fetch(rT, src + (ch0 + c) * GDN_BLKS * 3 * GDN_FRAG, (w & 1) * 9);
-    };
-    const auto fetch_kt = [&](int c) {
-        gdn_fetch(rKT, a.kt + (ck0 + c) * DT * 2 * GDN_FRAG, w * KTN);
-        gdn_fetch(rQT, a.qt + (ck0 + c) * DT * 2 * GDN_FRAG, w * KTN);
-    };
-    const auto stage_k = [&](int par) {
-        gdn_stage(sK, w * KTN, rK);
+    const auto fetch_t = [&](int c) { gdn_fetch_turns<NW>(rT, a.tf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
+    const auto fetch_p = [&](int c) { gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
+    const auto stage_kq = [&](int par) {
+        gdn_stage(sK, w * C::FPW, rK);
+        gdn_stage(sQ, w * C::FPW, rQ);
         if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
-    };
-    const auto stage_t = [&]() { gdn_stage(sT, w * 9, rT); };
-    const auto stage_kt = [&]() {
-        gdn_stage(sKT, w * KTN, rKT);
-        gdn_stage(sQT, w * KTN, rQT);
+        if (NW == 2 && w == 0) sV[(par * 3 + 2) * 64 + lane] = rB;
     };
 
     if (nc > 0) {
-        fetch_k(nc - 1);
+        fetch_kq(nc - 1);
         fetch_y(nc - 1);
         fetch_t(nc - 1);
-        fetch_kt(nc - 1);
-        stage_k((nc - 1) & 1);
-        stage_t();
-        stage_kt();
+        fetch_p(nc - 1);
+        give_state();
+        stage_kq((nc - 1) & 1);
+        gdn_stage_turns<NW>(sT, 18, w, rT);
+        gdn_stage_turns<NW>(sP, 18, w, rP);
         const int c1 = max(nc - 2, 0);
-        fetch_k(c1);
+        fetch_p(c1);
         fetch_t(c1);
-        fetch_kt(c1);
+        fetch_kq(c1);
         __syncthreads();
     }
     for (int c = nc - 1; c >= 0; --c) {
-        const int t0 = c * GDN_C, left = len - t0, next = max(c - 2, 0);
+        const int left = len - c * GDN_C, next = max(c - 2, 0);
         const float* vec = sV + (c & 1) * 3 * 64;
-        const auto rbuf = gdn_buf(dvp + (size_t)t0 * a.dv, (size_t)min(left, GDN_C) * a.dv * 4);
-        gdn_store_state(S, a.dS + (ch0 + c) * sn, a.dk, a.dv, co);
-        sdm_f32x4 dE[4], Y[4], dR[4];
+        const auto rbuf = gdn_buf(a.dvv + ((size_t)bh * a.T + (size_t)c * GDN_C) * a.dv, (size_t)min(left, GDN_C) * a.dv * 4);
+        gdn_store_state(S, a.dS + (ch0 + c) * sn, h * KTN, a.dk, a.dv, co);
+        sdm_f32x4 dE[2], dR[2], Y[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            dE[m] = dR[m] = zero;
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int r = 0; r < 4; ++r) Y[m][r] = rY[m][r];
+#pragma unroll
+        for (int m = 0; m < 2; ++m) dE[m] = dR[m] = zero;
+        // dE = C K dS1 + P^T dY of this half's tokens
+#pragma unroll
+        for (int i = 0; i < KTN; ++i) {
+            const int kb = i < KH ? h * KH + i : (1 - h) * KH + i - KH;
+            const GdnFrag<3> s = i < KH ? sf[i < KH ? i : 0] : gdn_load_frag<3>(xS, kb);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<1>(sK, (2 * h + m) * KTN + kb), s, dE[m]);
         }
 #pragma unroll
-        for (int kb = 0; kb < KTN; ++kb) {
-            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) dE[m] = gdn_mm(gdn_load_frag<1>(sK, m * KTN + kb), s, dE[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f en = ld4(vec + 64 + gdn_row(m, 4 * g));
+        for (int m = 0; m < 2; ++m) {
+            const v4f en = ld4(vec + 64 + gdn_row(2 * h + m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) dE[m][r] *= en[r];
         }
-        __syncthreads();
-        stage_k((c + 1) & 1);
-        fetch_y(max(c - 1, 0));
-        fetch_k(next);
+        if (h == 0) {
+            const GdnFrag<3> y = gdn_stack(Y[0], Y[1]);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
+            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_up_blk(m, 0)), y, dE[m]);
+        }
+        {
+            const GdnFrag<3> y = gdn_stack(Y[2], Y[3]);
 #pragma unroll
-            for (int m = 0; m < 2 * kb + 2; ++m) dE[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_up_blk(m, kb)), f, dE[m]);
+            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<3>(sP, h ? 4 + m : 2 * m + 1), y, dE[m]);
         }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f be = ld4(vec + 128 + gdn_row(m, 4 * g));
+        for (int m = 0; m < 2; ++m) {
+            const v4f be = ld4(vec + 128 + gdn_row(2 * h + m, 4 * g));
 #pragma unroll
             for (int r = 0; r < 4; ++r) dE[m][r] *= be[r];
         }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(dE[2 * kb], dE[2 * kb + 1]);
-#pragma unroll
-            for (int m = 0; m < 2 * kb + 2; ++m) dR[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_up_blk(m, kb)), f, dR[m]);
-        }
+        const GdnFrag<3> ff = gdn_stack(dE[0], dE[1]);
+        if (h == 1) gdn_store_frag<3>(xF, 0, ff);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const v4f gam = ld4(vec + gdn_row(m, 4 * g));
 #pragma unroll
+            for (int r = 0; r < 4; ++r) Y[m][r] *= gam[r];
+        }
+        const GdnFrag<3> y0 = gdn_stack(Y[0], Y[1]), y1 = gdn_stack(Y[2], Y[3]);
+        __syncthreads();
+        gdn_stage_turns<NW>(sP, 18, w, rP);
+        fetch_y(max(c - 1, 0));
+        fetch_p(next);
+        // dR = T'^T F
+        if (h == 0) {
+            const GdnFrag<3> fb = gdn_load_frag<3>(xF, 0);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                dR[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_up_blk(m, 0)), ff, dR[m]);
+                dR[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_up_blk(m, 1)), fb, dR[m]);
+            }
+        } else {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) dR[m] = gdn_mm(gdn_load_frag<3>(sT, gdn_up_blk(2 + m, 1)), ff, dR[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const v4f gam = ld4(vec + gdn_row(2 * h + m, 4 * g));
+#pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                gdn_stf(rbuf, t * a.dv * 4 + co, dR[m][r]);
+                gdn_stf(rbuf, gdn_row(2 * h + m, 4 * g + r) * a.dv * 4 + co, dR[m][r]);
                 dR[m][r] *= -gam[r];
-                Y[m][r] *= gam[r];
             }
         }
+        const GdnFrag<3> nf = gdn_stack(dR[0], dR[1]);
+        gdn_store_frag<3>(h ? xB : xA, 0, nf);
         const float last = vec[63];
         __syncthreads();
-        stage_t();
+        gdn_stage_turns<NW>(sT, 18, w, rT);
         fetch_t(next);
+        // dS0 = gamma dS1 + Q^T (G dY) - K^T (G dR)
+        {
+            const GdnFrag<3> no = gdn_load_frag<3>(h ? xA : xB, 0);
 #pragma unroll
-        for (int d = 0; d < DT; ++d) S[d] *= last;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> fr = gdn_stack(dR[2 * kb], dR[2 * kb + 1]);
-            const GdnFrag<3> fy = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                S[d] = gdn_mm(gdn_load_frag<1>(sKT, d * 2 + kb), fr, S[d]);
-                S[d] = gdn_mm(gdn_load_frag<1>(sQT, d * 2 + kb), fy, S[d]);
+            for (int d = 0; d < KTN; ++d) {
+                S[d] *= last;
+                S[d] = gdn_mm(gdn_turned_frag<KTN>(sQ, h * KTN + d, 0), y0, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN>(sQ, h * KTN + d, 1), y1, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, h), nf, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, 1 - h), no, S[d]);
             }
         }
+        give_state();
         __syncthreads();
-        stage_kt();
-        fetch_kt(next);
+        stage_kq((c + 1) & 1);
+        fetch_kq(next);
+        __syncthreads();
     }
-    if (a.dstate0) gdn_store_state(S, a.dstate0 + bh * sn, a.dk, a.dv, co);
+    if (a.dstate0) gdn_store_state(S, a.dstate0 + bh * sn, h * KTN, a.dk, a.dv, co);
 }
 
 template <int KTN>
-hipError_t launch_adjoint_staged(const GdnArgs& a, hipStream_t st) {
-    const auto kfn = gdn_adjoint_staged_kernel<KTN>;
-    constexpr size_t lds = (size_t)(12 * KTN + 36) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
-    hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+hipError_t launch_adjoint_halves(const GdnArgs& a, hipStream_t st) {
+    using C = AdjCfg<KTN>;
+    const auto kfn = gdn_adjoint_halves_kernel<KTN>;
+    hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
     if (e != hipSuccess) return e;
-    kfn<<<dim3((a.dv + 63) / 64 * a.B * a.H), 256, lds, st>>>(a);
+    kfn<<<dim3((a.dv + 16 * C::NCT - 1) / (16 * C::NCT) * a.B * a.H), C::NW * 64, C::LDS, st>>>(a);
     return hipGetLastError();
 }
 
 // ---------------------------------------------------------------- gradients
 constexpr int LD = 68;
-// bytes of the staged fragments, or of the two 64x64 matrices that take their place
-constexpr size_t grads_stage(int ktn) {
-    const size_t stage = (size_t)(4 * ktn + 4) * 3 * GDN_FRAG * 2, pairs = (size_t)2 * 64 * LD * 4;
+// bytes of the staged fragments, or of what takes their place: two 64x64 matrices and, of bf16
+// inputs, the fragments of K and Q
+constexpr size_t grads_stage(int ktn, bool bf) {
+    const size_t stage = (size_t)(4 * ktn + 4) * 3 * GDN_FRAG * 2,
+                 pairs = (size_t)2 * 64 * LD * 4 + (bf ? (size_t)8 * ktn * GDN_FRAG * 2 : 0);
     return stage > pairs ? stage : pairs;
 }
 
@@ -335,7 +381,9 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
     uint16_t* sX = sD + DT * 3 * GDN_FRAG;                             // [4][3]
     float* mQ = reinterpret_cast<float*>(smem);                        // after the products, in their place
     float* mB = mQ + 64 * LD;
-    float* mP = reinterpret_cast<float*>(smem + grads_stage(KTN));
+    uint16_t* sK = reinterpret_cast<uint16_t*>(mB + 64 * LD);          // [4][KTN] fragments (bf16)
+    uint16_t* sQ = sK + 4 * KTN * GDN_FRAG;
+    float* mP = reinterpret_cast<float*>(smem + grads_stage(KTN, NT == 1));
     float* mN = mP + 64 * LD;
     float* sV = mN + 64 * LD;                                          // the chunk's vectors
     const float *vlh = sV + GDN_V_LHI * 64, *vll = sV + GDN_V_LLO * 64, *vb = sV + GDN_V_BETA * 64;
@@ -344,13 +392,11 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
     const int c = blockIdx.x, b = blockIdx.y / a.Hk, hk = blockIdx.y % a.Hk, G = a.H / a.Hk;
     const int len = gdn_len(a, b), t0 = c * GDN_C, left = len - t0;
     if (left <= 0) return;
-    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15,
-              g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int w = wave & 3, half = wave >> 2, d0 = half * DH;
     const size_t tq = (size_t)(b * a.Hk + hk) * a.T + t0;
     const size_t ck = (size_t)(b * a.Hk + hk) * a.nC + c;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-    const int arow = gdn_row(w, r16);         // the A operands' token; in the C layout gdn_row(w, 4 g + r)
     const int wk = w >> 1;                    // the 32 tokens that hold the wave's
     const int dvb = (a.dv + 31) / 32;
     const uint32_t rows_bytes = (uint32_t)min(left, GDN_C) * a.dv * 4, st_bytes = (uint32_t)a.dk * a.dv * 4;
@@ -359,13 +405,15 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
     const auto bdq = gdn_buf(a.dq + tq * a.dk, kq_n * 4), bdk = gdn_buf(a.dkk + tq * a.dk, kq_n * 4);
 
     for (int hg = 0; hg < G; ++hg) {
+        // Said to change, so that addresses and masks are formed where they are used: the same
+        // for every head, they would be kept across the products (and spill, 16 KB a wave).
+        int lane = lane_id();
+        asm volatile("" : "+v"(lane));
+        const int tid = wave * 64 + lane, r16 = lane & 15, g = lane >> 4;
+        const int arow = gdn_row(w, r16);     // the A operands' token; in the C layout gdn_row(w, 4 g + r)
         const int bh = b * a.H + hk * G + hg;
         const size_t ch = (size_t)bh * a.nC + c, tv = (size_t)bh * a.T + t0;
         const float* vec = a.vec + ch * GDN_VEC * 64;
-        // the fragments of k and q are the same for every head; said to change, they are
-        // read after the products and not kept in registers across them
-        const uint16_t *kth = a.kt, *qth = a.qt;
-        asm volatile("" : "+s"(kth), "+s"(qth));
         const auto bS = gdn_buf(a.saved_S + ch * a.dk * a.dv, st_bytes), bD = gdn_buf(a.dS + ch * a.dk * a.dv, st_bytes);
         const auto bX = gdn_buf(a.saved_X + tv * a.dv, rows_bytes), bY = gdn_buf(a.dy + tv * a.dv, rows_bytes),
                    bR = gdn_buf(a.dvv + tv * a.dv, rows_bytes);
@@ -426,17 +474,15 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
         __builtin_amdgcn_sched_barrier(0);
         through = wave_sum(through);
         if (lane == 0) rThr[wave] = through;
-        // everything the rest reads from memory, in one batch: the fragments of K^T and Q^T
-        // (this wave's own tokens are eight of the depths each lane holds) and P or N
-        GdnFrag<NT> fk[DH][2], fq[DH][2];
+        // everything the rest reads from memory, in one batch: K and Q of a bf16 input (their
+        // fragments go to LDS, where they are turned), and P or N
         float pn[4][4];
-#pragma unroll
-        for (int d = 0; d < DH; ++d)
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                fk[d][kb] = gdn_load_frag<NT>(kth, (ck * DT + d0 + d) * 2 + kb);
-                fq[d][kb] = gdn_load_frag<NT>(qth, (ck * DT + d0 + d) * 2 + kb);
-            }
+        constexpr int FPW = KTN / 2;          // fragments of K and of Q that a wave moves
+        u4v rK[FPW], rQ[FPW];
+        if constexpr (NT == 1) {
+            gdn_fetch_rows<KTN>(rK, static_cast<const bf16_t*>(a.k) + tq * a.dk, wave * FPW, left, a.dk);
+            gdn_fetch_rows<KTN>(rQ, static_cast<const bf16_t*>(a.q) + tq * a.dk, wave * FPW, left, a.dk);
+        }
         {
             const auto bpn = gdn_buf((half == 0 ? a.pm : a.nm) + ch * 64 * 64, 64 * 64 * 4);
 #pragma unroll
@@ -445,27 +491,42 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
                 for (int r = 0; r < 4; ++r)
                     pn[j][r] = gdn_ldf(bpn, (uint32_t)(gdn_row(w, 4 * g + r) * 64 + gdn_row(j, r16)) * 4);
         }
-        // rows of M against q and k; then dq (in M2) and dk (in M1) without the pairs' part
+        if constexpr (NT == 1) {
+            gdn_stage(sK, wave * FPW, rK);
+            gdn_stage(sQ, wave * FPW, rQ);
+            __syncthreads();
+        }
+        // K^T, Q^T: columns of tile d0 + d, depths 32 kb on
+        const auto kt = [&](int d, int kb) {
+            if constexpr (NT == 1) return gdn_turned_frag<KTN>(sK, d0 + d, kb);
+            else return gdn_load_frag<3>(a.kt, (ck * DT + d0 + d) * 2 + kb);
+        };
+        const auto qt = [&](int d, int kb) {
+            if constexpr (NT == 1) return gdn_turned_frag<KTN>(sQ, d0 + d, kb);
+            else return gdn_load_frag<3>(a.qt, (ck * DT + d0 + d) * 2 + kb);
+        };
+        // rows of M against q and k (this wave's own tokens are among the depths that each lane
+        // holds of a turned fragment); then dq (in M2) and dk (in M1) without the pairs' part
         const int i0 = gdn_row(w, 4 * g);
         const v4f gam = ld4(sV + GDN_V_GAM * 64 + i0), en = ld4(sV + GDN_V_END * 64 + i0), be = ld4(vb + i0);
         float pe[4] = {0.f, 0.f, 0.f, 0.f}, pf[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int d = 0; d < DH; ++d)
+        for (int d = 0; d < DH; ++d) {
+            const GdnFrag<NT> fk = kt(d, wk), fq = qt(d, wk);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float kv = 0.f, qv = 0.f;
 #pragma unroll
                 for (int x = NT - 1; x >= 0; --x) {
-                    // which of the two 32-token blocks, and which half of the lane's eight, is the wave's
-                    const sdm_bf16x8 tk = wk ? fk[d][1].t[x] : fk[d][0].t[x], tq8 = wk ? fq[d][1].t[x] : fq[d][0].t[x];
-                    kv += (float)(w & 1 ? tk[4 + r] : tk[r]);
-                    qv += (float)(w & 1 ? tq8[4 + r] : tq8[r]);
+                    kv += (float)(w & 1 ? fk.t[x][4 + r] : fk.t[x][r]);
+                    qv += (float)(w & 1 ? fq.t[x][4 + r] : fq.t[x][r]);
                 }
                 pe[r] = fmaf(kv, M1[d][r], pe[r]);
                 pf[r] = fmaf(qv, M2[d][r], fmaf(-kv, M3[d][r], pf[r]));
                 M2[d][r] *= gam[r];
                 M1[d][r] = be[r] * en[r] * M1[d][r] - gam[r] * M3[d][r];
             }
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
 #pragma unroll
@@ -552,9 +613,10 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
             const GdnFrag<3> fp = gdn_split(xp), ft = gdn_split(xt), fn = gdn_split(xn);
 #pragma unroll
             for (int d = 0; d < DH; ++d) {
-                M2[d] = gdn_mm(fp, fk[d][kb], M2[d]);
-                M1[d] = gdn_mm(ft, fq[d][kb], M1[d]);
-                M1[d] = gdn_mm(fn, fk[d][kb], M1[d]);
+                const GdnFrag<NT> fk = kt(d, kb);
+                M2[d] = gdn_mm(fp, fk, M2[d]);
+                M1[d] = gdn_mm(ft, qt(d, kb), M1[d]);
+                M1[d] = gdn_mm(fn, fk, M1[d]);
             }
         }
         // added to what the heads before left there (this thread's own stores)
@@ -595,7 +657,7 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
 
 template <typename VT, int KTN>
 hipError_t launch_grads(const GdnArgs& a, hipStream_t st) {
-    constexpr size_t lds = grads_stage(KTN) + (size_t)2 * 64 * LD * 4 + (GDN_VEC + 7) * 64 * 4;
+    constexpr size_t lds = grads_stage(KTN, sizeof(VT) == 2) + (size_t)2 * 64 * LD * 4 + (GDN_VEC + 7) * 64 * 4;
     const auto kfn = gdn_grads_kernel<VT, KTN>;
     hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
@@ -607,8 +669,7 @@ hipError_t launch_grads(const GdnArgs& a, hipStream_t st) {
 
 #define GDN_PICK(F)                                                      \
     do {                                                                 \
-        if (a.dk <= 32) F(1);                                            \
-        else if (a.dk <= 64) F(2);                                       \
+        if (a.dk <= 64) F(2);                                            \
         else if (a.dk <= 128) F(4);                                      \
         else F(8);                                                       \
     } while (0)
@@ -617,8 +678,8 @@ hipError_t sdm_launch_gdn_adjoint(const GdnArgs& a, hipStream_t st) {
     const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
 #define F(N)                                                                                 \
     do {                                                                                     \
-        if (a.in_dtype == SDM_DT_BF16) return launch_adjoint_staged<N>(a, st);               \
-        else gdn_adjoint_kernel<float, N><<<grid, 256, 0, st>>>(a);                          \
+        if (a.in_dtype == SDM_DT_BF16) return launch_adjoint_halves<N>(a, st);               \
+        else gdn_adjoint_kernel<N><<<grid, 256, 0, st>>>(a);                          \
     } while (0)
     GDN_PICK(F);
 #undef F
