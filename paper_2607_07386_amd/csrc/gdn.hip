@@ -136,43 +136,24 @@ __device__ __forceinline__ sdm_f32x4 lds_mm16(const float* A, int ar, int ac, co
 // One workgroup per (stream, chunk).  T' by blocks: the four 16x16 diagonal
 // blocks by substitution (a lane per column), then the blocks below them from
 // products, T'_21 = -T'_22 A_21 T'_11, first within each half, then between.
+// Everything is latency, so what counts is how many workgroups share a compute unit:
+// one 64x64 matrix in LDS serves A, then T' in its place, then P (23 KB, five workgroups).
 template <typename VT, int KTN, bool BWD>
 __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
     constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN;
-    __shared__ float M[64 * LD], Ti[64 * LD], P[64 * LD], W[32 * 36];
+    constexpr int KF = NT == 1 ? 4 * KTN * GDN_FRAG * 2 : 0, MW = (64 * LD + 32 * 36) * 4;
+    __shared__ __align__(16) unsigned char smem[KF > MW ? KF : MW];
     __shared__ float vlh[64], vll[64], vb[64];
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // fragments of K, until M takes their place
+    float* M = reinterpret_cast<float*>(smem);
+    float* W = M + 64 * LD;
     const int c = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh % a.H;
     const int G = a.H / a.Hk, hk = h / G;
     const int len = gdn_len(a, b), t0 = c * GDN_C;
     if (t0 >= len) return;
-    const int lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const size_t ch = (size_t)bh * a.nC + c;
 
-    if (w == 0) {
-        const int t = t0 + lane;
-        const bool ok = t < len;
-        float al = ok ? a.alpha[(size_t)bh * a.T + t] : 1.f;
-        al = al < GDN_ALPHA_MIN ? GDN_ALPHA_MIN : al;
-        const float be = ok ? a.beta[(size_t)bh * a.T + t] : 0.f;
-        double lam = log((double)al);
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const double o = __shfl_up(lam, m, 64);
-            if (lane >= m) lam += o;
-        }
-        const double end = __shfl(lam, 63, 64);
-        const float hi = (float)lam, lo = (float)(lam - (double)hi);
-        vlh[lane] = hi;
-        vll[lane] = lo;
-        vb[lane] = be;
-        float* vec = a.vec + ch * GDN_VEC * 64;
-        vec[GDN_V_LHI * 64 + lane] = hi;
-        vec[GDN_V_LLO * 64 + lane] = lo;
-        vec[GDN_V_GAM * 64 + lane] = (float)exp(lam);
-        vec[GDN_V_END * 64 + lane] = (float)exp(end - lam);
-        vec[GDN_V_BETA * 64 + lane] = be;
-        vec[GDN_V_ALPHA * 64 + lane] = al;
-    }
     // Gram matrices: this wave's 16 rows against the rows of blocks 0 .. w
     const size_t tq = (size_t)(b * a.Hk + hk) * a.T + t0;
     const VT* kp = static_cast<const VT*>(a.k) + tq * a.dk;
@@ -181,20 +162,73 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) kk[j] = qk[j] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
     const int row = 16 * w + r16;
-    for (int kb = 0; kb < KTN; ++kb) {
-        const bool ok = t0 + row < len;
-        const GdnFrag<NT> fk = gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, ok);
-        const GdnFrag<NT> fq = gdn_row_frag<NT>(qp + (size_t)row * a.dk, kb, a.dk, ok);
+    const bool ok = t0 + row < len;
+    const auto gates = [&]() {
+        const int t = t0 + lane;
+        const bool on = t < len;
+        float al = on ? a.alpha[(size_t)bh * a.T + t] : 1.f;
+        al = al < GDN_ALPHA_MIN ? GDN_ALPHA_MIN : al;
+        const float be = on ? a.beta[(size_t)bh * a.T + t] : 0.f;
+        // the logarithm in fp32 (its last bit counts as one more rounding of alpha), the sums
+        // and their differences beyond that
+        double lam = (double)logf(al);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) {
+            const double o = __shfl_up(lam, m, 64);
+            if (lane >= m) lam += o;
+        }
+        const double end = __shfl(lam, 63, 64);
+        const float hi = (float)lam, lo = (float)(lam - (double)hi), he = (float)(end - lam);
+        vlh[lane] = hi;
+        vll[lane] = lo;
+        vb[lane] = be;
+        float* vec = a.vec + ch * GDN_VEC * 64;
+        vec[GDN_V_LHI * 64 + lane] = hi;
+        vec[GDN_V_LLO * 64 + lane] = lo;
+        const float eh = expf(hi);
+        vec[GDN_V_GAM * 64 + lane] = fmaf(eh, lo, eh);
+        vec[GDN_V_END * 64 + lane] = expf(he);
+        vec[GDN_V_BETA * 64 + lane] = be;
+        vec[GDN_V_ALPHA * 64 + lane] = al;
+    };
+    if constexpr (NT == 1) {
+        GdnFrag<1> fk[KTN], fq[KTN];
+#pragma unroll
+        for (int kb = 0; kb < KTN; ++kb) {
+            fk[kb] = gdn_row_frag<1>(kp + (size_t)row * a.dk, kb, a.dk, ok);
+            fq[kb] = gdn_row_frag<1>(qp + (size_t)row * a.dk, kb, a.dk, ok);
+        }
+        if (w == 0) gates();      // has one block of the products to do, wave 3 four
+#pragma unroll
+        for (int kb = 0; kb < KTN; ++kb) gdn_store_frag<1>(sK, w * KTN + kb, fk[kb]);
+        __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             if (j > w) break;
-            const int rj = 16 * j + r16;
-            const GdnFrag<NT> fb = gdn_row_frag<NT>(kp + (size_t)rj * a.dk, kb, a.dk, t0 + rj < len);
-            kk[j] = gdn_mm(fk, fb, kk[j]);
-            qk[j] = gdn_mm(fq, fb, qk[j]);
+#pragma unroll
+            for (int kb = 0; kb < KTN; ++kb) {
+                const GdnFrag<1> fb = gdn_load_frag<1>(sK, j * KTN + kb);
+                kk[j] = gdn_mm(fk[kb], fb, kk[j]);
+                qk[j] = gdn_mm(fq[kb], fb, qk[j]);
+            }
+        }
+    } else {
+        if (w == 0) gates();
+        for (int kb = 0; kb < KTN; ++kb) {
+            const GdnFrag<NT> fk = gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, ok);
+            const GdnFrag<NT> fq = gdn_row_frag<NT>(qp + (size_t)row * a.dk, kb, a.dk, ok);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j > w) break;
+                const int rj = 16 * j + r16;
+                const GdnFrag<NT> fb = gdn_row_frag<NT>(kp + (size_t)rj * a.dk, kb, a.dk, t0 + rj < len);
+                kk[j] = gdn_mm(fk, fb, kk[j]);
+                qk[j] = gdn_mm(fq, fb, qk[j]);
+            }
         }
     }
     __syncthreads();
+    // M = N diag(beta), zeros above the diagonal; P stays in qk
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int cj = 16 * j + r16;
@@ -203,14 +237,13 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * w + 4 * g + r;
             float n = 0.f, p = 0.f;
-            if (cj <= i) {
-                const float d = gdn_decay(vlh[i], vll[i], hj, lj);
+            if (j <= w) {
+                const float d = gdn_decay(vlh[i], vll[i], hj, lj);   // may overflow above the diagonal
                 n = cj < i ? kk[j][r] * d : 0.f;
-                p = qk[j][r] * d;
+                p = cj <= i ? qk[j][r] * d : 0.f;
             }
             M[i * LD + cj] = n * bj;
-            P[i * LD + cj] = p;
-            Ti[i * LD + cj] = 0.f;
+            qk[j][r] = p;
             if constexpr (BWD) {
                 a.pm[(ch * 64 + i) * 64 + cj] = p;
                 a.nm[(ch * 64 + i) * 64 + cj] = n;
@@ -218,7 +251,7 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
         }
     }
     __syncthreads();
-    if (lane < 16) {   // diagonal block w, column `lane`
+    if (lane < 16) {   // diagonal block w, column `lane`, in place: the lanes read before any of them writes
         const int o = 16 * w;
         float x[16];
 #pragma unroll
@@ -227,56 +260,67 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
 #pragma unroll
             for (int l = 0; l < i; ++l) s = fmaf(-M[(o + i) * LD + o + l], x[l], s);
             x[i] = s;
-            Ti[(o + i) * LD + o + lane] = s;
         }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) M[(o + i) * LD + o + lane] = x[i];
     }
     __syncthreads();
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     if (w < 2) {       // W <- A_21 T'_11 within half w
-        const sdm_f32x4 t = lds_mm16(M, 32 * w + 16, 32 * w, Ti, 32 * w, 32 * w, LD, zero);
+        const sdm_f32x4 t = lds_mm16(M, 32 * w + 16, 32 * w, M, 32 * w, 32 * w, LD, zero);
 #pragma unroll
         for (int r = 0; r < 4; ++r) W[(16 * w + 4 * g + r) * 36 + r16] = t[r];
     }
     __syncthreads();
     if (w < 2) {
-        const sdm_f32x4 t = lds_mm16(Ti, 32 * w + 16, 32 * w + 16, W, 16 * w, 0, 36, zero);
+        const sdm_f32x4 t = lds_mm16(M, 32 * w + 16, 32 * w + 16, W, 16 * w, 0, 36, zero);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) Ti[(32 * w + 16 + 4 * g + r) * LD + 32 * w + r16] = -t[r];
+        for (int r = 0; r < 4; ++r) M[(32 * w + 16 + 4 * g + r) * LD + 32 * w + r16] = -t[r];
     }
     __syncthreads();
     {                  // between the halves: 32x32, a 16x16 tile per wave
         const int ti = w >> 1, tj = w & 1;
-        sdm_f32x4 t = lds_mm16(M, 32 + 16 * ti, 0, Ti, 0, 16 * tj, LD, zero);
-        t = lds_mm16(M, 32 + 16 * ti, 16, Ti, 16, 16 * tj, LD, t);
+        sdm_f32x4 t = lds_mm16(M, 32 + 16 * ti, 0, M, 0, 16 * tj, LD, zero);
+        t = lds_mm16(M, 32 + 16 * ti, 16, M, 16, 16 * tj, LD, t);
 #pragma unroll
         for (int r = 0; r < 4; ++r) W[(16 * ti + 4 * g + r) * 36 + 16 * tj + r16] = t[r];
         __syncthreads();
-        t = lds_mm16(Ti, 32 + 16 * ti, 32, W, 0, 16 * tj, 36, zero);
-        t = lds_mm16(Ti, 32 + 16 * ti, 48, W, 16, 16 * tj, 36, t);
+        t = lds_mm16(M, 32 + 16 * ti, 32, W, 0, 16 * tj, 36, zero);
+        t = lds_mm16(M, 32 + 16 * ti, 48, W, 16, 16 * tj, 36, t);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) Ti[(32 + 16 * ti + 4 * g + r) * LD + 16 * tj + r16] = -t[r];
+        for (int r = 0; r < 4; ++r) M[(32 + 16 * ti + 4 * g + r) * LD + 16 * tj + r16] = -t[r];
     }
     __syncthreads();
-    // fragments of T' and P (backward: of their transposes): 6 blocks each
-    for (int f = w; f < 2 * GDN_BLKS; f += 4) {
-        const int blk = f % GDN_BLKS;
-        const float* src = f < GDN_BLKS ? Ti : P;
-        int mt, kb;
-        if constexpr (BWD) {
-            mt = blk < 4 ? blk >> 1 : blk - 2;
-            kb = blk < 4 ? blk & 1 : 1;
-        } else {
-            mt = blk < 2 ? blk : 2 + ((blk - 2) >> 1);
-            kb = blk < 2 ? 0 : (blk - 2) & 1;
-        }
-        float x[8];
+    // fragments of T', then of P (backward: of their transposes), 6 blocks each
+    const auto blocks = [&](uint16_t* to) {
+        for (int blk = w; blk < GDN_BLKS; blk += 4) {
+            int mt, kb;
+            if constexpr (BWD) {
+                mt = blk < 4 ? blk >> 1 : blk - 2;
+                kb = blk < 4 ? blk & 1 : 1;
+            } else {
+                mt = blk < 2 ? blk : 2 + ((blk - 2) >> 1);
+                kb = blk < 2 ? 0 : (blk - 2) & 1;
+            }
+            float x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int rr = gdn_row(mt, r16), cc = 32 * kb + 8 * g + i;
-            x[i] = BWD ? src[cc * LD + rr] : src[rr * LD + cc];
+            for (int i = 0; i < 8; ++i) {
+                const int rr = gdn_row(mt, r16), cc = 32 * kb + 8 * g + i;
+                x[i] = BWD ? M[cc * LD + rr] : M[rr * LD + cc];
+            }
+            gdn_store_frag<3>(to, ch * GDN_BLKS + blk, gdn_split(x));
         }
-        gdn_store_frag<3>(f < GDN_BLKS ? a.tf : a.pf, ch * GDN_BLKS + blk, gdn_split(x));
-    }
+    };
+    blocks(a.tf);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) M[(16 * w + 4 * g + r) * LD + 16 * j + r16] = qk[j][r];
+    __syncthreads();
+    blocks(a.pf);
     // fp32: K^T (and Q^T) of the key head, rows of d_k, depth = tokens (bf16 scans turn K in LDS)
     if constexpr (NT == 3) {
         if (h % G) return;
