@@ -476,9 +476,9 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
 // other (the state's fragments, R and E of the first 32 tokens, E for the update)
 // passes through LDS.  The chunk's K, Q, T' and P are fetched into registers a chunk
 // ahead and staged once for the workgroup; K^T is K read with the transposing loads.
-template <int KTN>
+template <int KTN, int NCT_>
 struct ScanCfg {
-    static constexpr int NCT = KTN == 8 ? 2 : 4;       // column tiles of a workgroup
+    static constexpr int NCT = NCT_;                   // column tiles of a workgroup
     static constexpr int NW = 2 * NCT;
     static constexpr bool QD = KTN == 8;               // Q straight from memory: LDS is full
     static constexpr int FPW = 4 * KTN / NW;           // fragments of K (and Q) that a wave moves
@@ -488,9 +488,9 @@ struct ScanCfg {
         (size_t)(4 * KTN * (QD ? 1 : 2) + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
 };
 
-template <int KTN, bool SAVE>
-__global__ __launch_bounds__(ScanCfg<KTN>::NW * 64) void gdn_scan_halves_kernel(GdnArgs a) {
-    using C = ScanCfg<KTN>;
+template <int KTN, int NCT, bool SAVE>
+__global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a) {
+    using C = ScanCfg<KTN, NCT>;
     constexpr int NW = C::NW, KH = KTN / 2;            // KH: 32-row blocks of the state per wave
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN]
@@ -532,12 +532,13 @@ __global__ __launch_bounds__(ScanCfg<KTN>::NW * 64) void gdn_scan_halves_kernel(
     };
 
     u4v rK[C::FPW], rQ[C::FPW], rT[C::TPW], rP[C::TPW];
-    float rV, V[2][4];
+    float rV, rB = 0.f, V[2][4];                            // rB: beta where the workgroup has two waves
     const auto fetch_k = [&](int c) { gdn_fetch_rows<KTN>(rK, kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk); };
     const auto fetch_q = [&](int c) {
         if constexpr (!C::QD) gdn_fetch_rows<KTN>(rQ, qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
         const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // waves 3 on repeat wave 2
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
+        if constexpr (NW == 2) rB = a.vec[(ch0 + c) * GDN_VEC * 64 + GDN_V_BETA * 64 + lane];
     };
     const auto fetch_v = [&](int c) {
         const int t0 = c * GDN_C;
@@ -553,6 +554,7 @@ __global__ __launch_bounds__(ScanCfg<KTN>::NW * 64) void gdn_scan_halves_kernel(
     const auto stage_q = [&](int par) {
         if constexpr (!C::QD) gdn_stage(sQ, w * C::FPW, rQ);
         if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
+        if (NW == 2 && w == 0) sV[(par * 3 + 2) * 64 + lane] = rB;
     };
 
     if (nc > 0) {
@@ -681,14 +683,25 @@ __global__ __launch_bounds__(ScanCfg<KTN>::NW * 64) void gdn_scan_halves_kernel(
     gdn_store_state(S, a.stateT + bh * sn, h * KTN, a.dk, a.dv, co);
 }
 
-template <int KTN, bool SAVE>
-hipError_t launch_scan_halves(const GdnArgs& a, hipStream_t st) {
-    using C = ScanCfg<KTN>;
-    const auto kfn = gdn_scan_halves_kernel<KTN, SAVE>;
+template <int KTN, int NCT, bool SAVE>
+hipError_t launch_scan_tiles(const GdnArgs& a, hipStream_t st) {
+    using C = ScanCfg<KTN, NCT>;
+    const auto kfn = gdn_scan_halves_kernel<KTN, NCT, SAVE>;
     hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
     if (e != hipSuccess) return e;
     kfn<<<dim3((a.dv + 16 * C::NCT - 1) / (16 * C::NCT) * a.B * a.H), C::NW * 64, C::LDS, st>>>(a);
     return hipGetLastError();
+}
+
+// Column tiles to a workgroup: as many as leave a workgroup to every compute unit. More
+// share one staging of the chunk, but also one LDS, whose reads then set the pace.
+template <int KTN, bool SAVE>
+hipError_t launch_scan_halves(const GdnArgs& a, hipStream_t st) {
+    const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
+    if constexpr (KTN < 8) {
+        if (tiles >= 4 * cus) return launch_scan_tiles<KTN, 4, SAVE>(a, st);
+    }
+    return tiles >= 2 * cus ? launch_scan_tiles<KTN, 2, SAVE>(a, st) : launch_scan_tiles<KTN, 1, SAVE>(a, st);
 }
 
 }  // namespace

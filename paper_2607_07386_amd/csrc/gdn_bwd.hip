@@ -150,9 +150,9 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
 // holds tokens 32 h .. + 31 and one half of the state's rows.  dY is read whole by both
 // (its part below needs no exchange); F = diag(beta) dE of the last 32 tokens and -G dR
 // pass through LDS.
-template <int KTN>
+template <int KTN, int NCT_>
 struct AdjCfg {
-    static constexpr int NCT = KTN == 8 ? 1 : 4;
+    static constexpr int NCT = NCT_;
     static constexpr int NW = 2 * NCT;
     static constexpr int FPW = 4 * KTN / NW;
     static constexpr int TPW = (18 + NW - 1) / NW;
@@ -160,9 +160,9 @@ struct AdjCfg {
     static constexpr size_t LDS = (size_t)(8 * KTN + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
 };
 
-template <int KTN>
-__global__ __launch_bounds__(AdjCfg<KTN>::NW * 64) void gdn_adjoint_halves_kernel(GdnArgs a) {
-    using C = AdjCfg<KTN>;
+template <int KTN, int NCT>
+__global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArgs a) {
+    using C = AdjCfg<KTN, NCT>;
     constexpr int NW = C::NW, KH = KTN / 2;
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN]
@@ -345,14 +345,24 @@ __global__ __launch_bounds__(AdjCfg<KTN>::NW * 64) void gdn_adjoint_halves_kerne
     if (a.dstate0) gdn_store_state(S, a.dstate0 + bh * sn, h * KTN, a.dk, a.dv, co);
 }
 
-template <int KTN>
-hipError_t launch_adjoint_halves(const GdnArgs& a, hipStream_t st) {
-    using C = AdjCfg<KTN>;
-    const auto kfn = gdn_adjoint_halves_kernel<KTN>;
+template <int KTN, int NCT>
+hipError_t launch_adjoint_tiles(const GdnArgs& a, hipStream_t st) {
+    using C = AdjCfg<KTN, NCT>;
+    const auto kfn = gdn_adjoint_halves_kernel<KTN, NCT>;
     hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
     if (e != hipSuccess) return e;
     kfn<<<dim3((a.dv + 16 * C::NCT - 1) / (16 * C::NCT) * a.B * a.H), C::NW * 64, C::LDS, st>>>(a);
     return hipGetLastError();
+}
+// column tiles to a workgroup as in the forward scan
+template <int KTN>
+hipError_t launch_adjoint_halves(const GdnArgs& a, hipStream_t st) {
+    const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
+    if constexpr (KTN < 8) {
+        if (tiles >= 4 * cus) return launch_adjoint_tiles<KTN, 4>(a, st);
+        if (tiles >= 2 * cus) return launch_adjoint_tiles<KTN, 2>(a, st);
+    }
+    return launch_adjoint_tiles<KTN, 1>(a, st);
 }
 
 // ---------------------------------------------------------------- gradients
