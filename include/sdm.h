@@ -466,7 +466,8 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *   residual  [B, T, N] in y_dtype or NULL; only with y_heads = 0.
  *   y         out [B, T, N], or head-major [B, y_heads, T, N / y_heads] as the
  *             recurrences read it, in y_dtype: w's type, or fp32.
- *   z         optional out, laid out and typed as y, for sdm_linear_bwd.
+ *   z         optional out, laid out and typed as y, for sdm_linear_bwd;  z_rest  optional
+ *             out beside a bf16 z: what its rounding left, in bf16.
  * Sums are fp32; bf16 products are exact, fp32 ones fp32.  Sums over split
  * depths are added in a fixed order: results are the same from run to run.
  * y may be residual; no other output may overlap an input.
@@ -480,17 +481,19 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *   dy        laid out as y, in dy_dtype: w's type, or fp32 (as the recurrences'
  *             backwards write their gradients).  dz is rounded to w's type, in which
  *             it enters the products; dbias sums it in fp32 before that.
- *   z         as sdm_linear wrote it (z_dtype); NULL with act 0.
+ *   z, z_rest as sdm_linear wrote them (z_dtype); NULL with act 0.  With z_rest the
+ *             activation's slope is taken at z to 2^-17; without it at the rounded z, whose
+ *             2^-9 shows in dbias (the products round dz to bf16 anyway).
  *   dx        optional out, laid out and typed as x;  dw  optional out [N, K] in
  *             w_dtype;  dbias  optional out [N] fp32.
  *   workspace  at least sdm_linear_bwd_workspace_bytes() bytes, 256-B aligned.
  * ---------------------------------------------------------------------- */
 int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const float* bias, int act,
                const void* residual, int B, int T, int K, int N, int y_heads, void* y, int y_dtype, void* z,
-               void* workspace, size_t ws_bytes, void* stream);
+               void* z_rest, void* workspace, size_t ws_bytes, void* stream);
 size_t sdm_linear_workspace_bytes(int x_dtype, int w_dtype, int B, int T, int K, int N);
-int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const void* z, int z_dtype,
-                   int act, const void* dy, int dy_dtype, int B, int T, int K, int N, int y_heads, void* dx, void* dw,
+int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const void* z,
+                   const void* z_rest, int z_dtype, int act, const void* dy, int dy_dtype, int B, int T, int K, int N, int y_heads, void* dx, void* dw,
                    float* dbias, void* workspace, size_t ws_bytes, void* stream);
 size_t sdm_linear_bwd_workspace_bytes(int x_dtype, int w_dtype, int act, int dy_dtype, int B, int T, int K, int N,
                                       int y_heads);

@@ -32,18 +32,21 @@ struct LinGemm {
     // products of parts of total order <= 2 are added up
     int combos;
     int64_t plane_a, plane_b;
-    // out = act(C + bias) + residual, pre = C + bias; both laid out as `out`
+    // out = act(C + bias) + residual, pre = C + bias, rest = what pre's rounding to bf16 left; all laid out
+    // and typed as `out`
     LinMat out;
     void* pre;
+    void* rest;
     const float* bias;
     const void* residual;
     int act;
-    // depth split over `split` workgroups: fp32 partial sums [split][I][J], added up by a second launch
+    // depth split over `split` workgroups: fp32 partial sums [split][I][LIN_UP8(J)], added up by a second launch
     int split;
     bool big;             // 256 x 256 tiles, else 128 x 128
     float* part;
 };
 
+#define LIN_UP8(x) (((x) + 7) / 8 * 8)
 struct LinPlan {
     bool big;
     int split;
@@ -57,8 +60,8 @@ hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st);
 // an fp32 matrix as np bf16 planes [rows][ld] (np 1: rounded, 3: the parts), zeros past its end
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st);
 // dz = dy act'(z) as np planes [rows][ld], zeros past M and N, and dbias = its column sums
-// (through parts [sdm_linear_dz_parts(M)][N] added in order).  dz may be NULL.
-int sdm_linear_dz_parts(int M);
-hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int np, int rows, int ld,
+// (through parts [sdm_linear_dz_parts(rows, ld)][N] added in order).  dz and rest may be NULL.
+int sdm_linear_dz_parts(int rows, int ld);
+hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, const void* rest, int z_dtype, int act, int np, int rows, int ld,
                                 void* dz, float* part, float* dbias, hipStream_t st);
 hipError_t sdm_launch_linear_zero(void* p, size_t words, hipStream_t st);

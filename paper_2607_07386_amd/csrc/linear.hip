@@ -58,6 +58,7 @@ __device__ __forceinline__ void st_any(void* p, int dtype, int64_t i, float x) {
 __device__ __forceinline__ void lin_store(const LinGemm& g, int64_t o, int j, float c) {
     if (g.bias) c += g.bias[j];
     if (g.pre) st_any(g.pre, g.out.dtype, o, c);
+    if (g.rest) st_any(g.rest, g.out.dtype, o, c - (float)(__bf16)c);
     c = lin_act(c, g.act);
     if (g.residual) c += ld_any(g.residual, g.out.dtype, o);
     st_any(const_cast<void*>(g.out.p), g.out.dtype, o, c);
@@ -107,6 +108,12 @@ __device__ __forceinline__ void lin_store8(const LinGemm& g, bool wide, int64_t 
 #pragma unroll
     for (int i = 0; i < 8; ++i) c[i] += b[i];
     if (g.pre) st8(g.pre, g.out.dtype, o, c);
+    if (g.rest) {
+        float r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = c[i] - (float)(__bf16)c[i];
+        st8(g.rest, g.out.dtype, o, r);
+    }
     if (g.act == 1) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) c[i] = lin_act(c[i], 1);
@@ -129,23 +136,20 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinGemm g) {
     const int j = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
     if (j >= g.J) return;
     const bool wide = lin_wide(g);
-    const size_t n = (size_t)g.I * g.J;
+    const size_t n = (size_t)g.I * LIN_UP8(g.J);
     float b[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) b[i] = g.bias && j + i < g.J ? g.bias[j + i] : 0.f;
     for (int row = blockIdx.y * 8 + (threadIdx.x >> 5); row < g.I; row += gridDim.y * 8) {
-        const float* p = g.part + (size_t)row * g.J + j;
+        const float* p = g.part + (size_t)row * LIN_UP8(g.J) + j;
         float c[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
         for (int s = 0; s < g.split; ++s) {
-            if (wide) {
-                const v4f u = ld4(p + s * n), v = ld4(p + s * n + 4);
+            const v4f u = ld4(p + s * n), v = ld4(p + s * n + 4);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    c[i] += u[i];
-                    c[4 + i] += v[i];
-                }
-            } else {
-                for (int i = 0; i < 8 && j + i < g.J; ++i) c[i] += p[s * n + i];
+            for (int i = 0; i < 4; ++i) {
+                c[i] += u[i];
+                c[4 + i] += v[i];
             }
         }
         lin_store8(g, wide, mat_row(g.out, row), j, b, c);
@@ -384,13 +388,9 @@ __global__ __launch_bounds__(WR* WC * 64) void linear_tile_kernel(LinGemm g, int
                 c[4 + x] = v[x];
             }
             if (g.split > 1) {
-                float* o = g.part + ((size_t)blockIdx.y * g.I + oi) * g.J + oj;
-                if (wide) {
-                    st4(o, u);
-                    st4(o + 4, v);
-                } else {
-                    for (int x = 0; x < 8 && oj + x < g.J; ++x) o[x] = c[x];
-                }
+                float* o = g.part + ((size_t)blockIdx.y * g.I + oi) * LIN_UP8(g.J) + oj;
+                st4(o, u);
+                st4(o + 4, v);
             } else lin_store8(g, wide, mat_row(g.out, oi), oj, bias, c);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -534,11 +534,11 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(LinMat m, int rows, i
 }
 
 // dz = dy act'(z) as planes [rows][ld] (zeros past M and N) and its column sums over this
-// workgroup's rows: eight columns a thread, 8 rows at a time.
-constexpr int DZ_ROWS = 128;
+// `per` rows: eight columns a thread, 8 rows at a time.
 template <int NP>
-__global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z, int z_dtype, int act, int rows,
-                                                        int ld, bf16_t* dz, int64_t plane, float* part) {
+__global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z, const void* rest, int z_dtype, int act,
+                                                        int rows, int per, int ld, bf16_t* dz, int64_t plane,
+                                                        float* part) {
     __shared__ float red[8][256];
     const int cl = threadIdx.x & 31, rg = threadIdx.x >> 5, c = (blockIdx.x * 32 + cl) * 8;
     const bool wide = dy.cols % 8 == 0 && dy.d % 8 == 0;
@@ -547,8 +547,8 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z
     for (int i = 0; i < 8; ++i) cols[i] = c + i < dy.cols ? mat_col(dy, c + i) : 0;
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (c < ld) {
-        const int m1 = min(rows, (int)(blockIdx.y + 1) * DZ_ROWS);
-        for (int m = blockIdx.y * DZ_ROWS + rg; m < m1; m += 8) {
+        const int m1 = min(rows, (int)(blockIdx.y + 1) * per);
+        for (int m = blockIdx.y * per + rg; m < m1; m += 8) {
             float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (m < dy.rows && c < dy.cols) {
                 const int64_t ro = mat_row(dy, m);
@@ -557,6 +557,12 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z
                     if (act) {
                         float zz[8];
                         ld8(z, z_dtype, ro + cols[0], zz);
+                        if (rest) {
+                            float zr[8];
+                            ld8(rest, z_dtype, ro + cols[0], zr);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) zz[i] += zr[i];
+                        }
 #pragma unroll
                         for (int i = 0; i < 8; ++i) x[i] *= act == 1 ? lin_act_slope(zz[i], 1) : lin_act_slope(zz[i], 2);
                     }
@@ -565,7 +571,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z
                     for (int i = 0; i < 8; ++i) {
                         const int64_t o = ro + cols[i];   // a column past the end reads the first one
                         x[i] = ld_any(dy.p, dy.dtype, o);
-                        if (act) x[i] *= lin_act_slope(ld_any(z, z_dtype, o), act);
+                        if (act) x[i] *= lin_act_slope(ld_any(z, z_dtype, o) + (rest ? ld_any(rest, z_dtype, o) : 0.f), act);
                         x[i] = c + i < dy.cols ? x[i] : 0.f;
                     }
                 }
@@ -656,17 +662,23 @@ hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, vo
     return hipGetLastError();
 }
 
-int sdm_linear_dz_parts(int M) { return (M + 63) / 64 * 64 / DZ_ROWS + 1; }
+// Rows of a dz workgroup (a multiple of 8, at most 128): four workgroups to a compute unit where
+// the matrix is large enough.
+static int dz_rows(int rows, int ld) {
+    const int64_t want = 4 * (sdm_device_simds() / 4), cb = (ld + 255) / 256;
+    return (int)std::max<int64_t>(8, std::min<int64_t>(128, (int64_t)rows * cb / want / 8 * 8));
+}
+int sdm_linear_dz_parts(int rows, int ld) { return (rows + dz_rows(rows, ld) - 1) / dz_rows(rows, ld); }
 
-hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, int z_dtype, int act, int np, int rows, int ld,
-                                void* dz, float* part, float* dbias, hipStream_t st) {
-    const int parts = (rows + DZ_ROWS - 1) / DZ_ROWS;
+hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, const void* rest, int z_dtype, int act, int np,
+                                int rows, int ld, void* dz, float* part, float* dbias, hipStream_t st) {
+    const int per = dz_rows(rows, ld), parts = sdm_linear_dz_parts(rows, ld);
     const dim3 grid((ld + 255) / 256, parts);
     float* p = dbias ? part : nullptr;
     bf16_t* o = static_cast<bf16_t*>(dz);
     const int64_t plane = (int64_t)rows * ld;
-    if (np == 3) linear_dz_kernel<3><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, rows, ld, o, plane, p);
-    else linear_dz_kernel<1><<<grid, 256, 0, st>>>(dy, z, z_dtype, act, rows, ld, o, plane, p);
+    if (np == 3) linear_dz_kernel<3><<<grid, 256, 0, st>>>(dy, z, rest, z_dtype, act, rows, per, ld, o, plane, p);
+    else linear_dz_kernel<1><<<grid, 256, 0, st>>>(dy, z, rest, z_dtype, act, rows, per, ld, o, plane, p);
     if (dbias) linear_colsum_kernel<<<(dy.cols + 31) / 32, 256, 0, st>>>(part, parts, dy.cols, dbias);
     return hipGetLastError();
 }

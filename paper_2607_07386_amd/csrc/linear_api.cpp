@@ -67,7 +67,7 @@ struct Ws {
     }
 };
 size_t planes(int np, int rows, int cols) { return (size_t)np * up64(rows) * up64(cols) * 2; }
-size_t split_bytes(const LinPlan& p, int I, int J) { return p.split > 1 ? (size_t)p.split * I * J * 4 : 0; }
+size_t split_bytes(const LinPlan& p, int I, int J) { return p.split > 1 ? (size_t)p.split * I * LIN_UP8(J) * 4 : 0; }
 
 Ws fwd_ws(int x_dtype, int w_dtype, int M, int K, int N) {
     Ws s;
@@ -85,7 +85,7 @@ Ws bwd_ws(int x_dtype, int w_dtype, int act, int dy_dtype, int y_heads, int M, i
     if (!s.direct) s.dz = s.take(planes(np, M, N));
     if (x_dtype == SDM_F32) s.x = s.take(planes(np, M, K));
     if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
-    s.parts = s.take((size_t)sdm_linear_dz_parts(M) * N * 4);
+    s.parts = s.take((size_t)sdm_linear_dz_parts(up64(M), up64(N)) * N * 4);
     s.px = sdm_linear_plan(M, K, steps_of(N, w_dtype));
     s.pw = sdm_linear_plan(N, K, steps_of(M, w_dtype));
     s.split = s.take(std::max(split_bytes(s.px, M, K), split_bytes(s.pw, N, K)));
@@ -109,17 +109,19 @@ size_t sdm_linear_workspace_bytes(int x_dtype, int w_dtype, int B, int T, int K,
 
 int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const float* bias, int act,
                const void* residual, int B, int T, int K, int N, int y_heads, void* y, int y_dtype, void* z,
-               void* workspace, size_t ws_bytes, void* stream) {
+               void* z_rest, void* workspace, size_t ws_bytes, void* stream) {
     sdm_set_error(SDM_OK, "");
     if (const char* m = bad_sizes(x_dtype, x_heads, w_dtype, act, B, T, K, N, y_heads))
         return fail(SDM_ERR_INVALID_ARG, m);
     if (const char* m = too_large(B, T, K, N)) return fail(SDM_ERR_UNSUPPORTED, m);
     if (!valid_dtype(y_dtype) || (w_dtype == SDM_F32 && y_dtype != SDM_F32))
         return fail(SDM_ERR_INVALID_ARG, "y_dtype must be w's or SDM_F32");
+    if (z_rest && (!z || y_dtype != SDM_BF16)) return fail(SDM_ERR_INVALID_ARG, "z_rest goes with a bf16 z");
     if (residual && y_heads) return fail(SDM_ERR_INVALID_ARG, "a residual needs a flat y (y_heads 0)");
     if ((int64_t)B * T == 0) return SDM_OK;
     if (!x || !w || !y) return fail(SDM_ERR_INVALID_ARG, "null pointer");
-    if (!aligned(x, 16) || !aligned(w, 16) || !aligned(y, 16) || !aligned(z, 16) || !aligned(residual, 16) ||
+    if (!aligned(x, 16) || !aligned(w, 16) || !aligned(y, 16) || !aligned(z, 16) || !aligned(z_rest, 16) ||
+        !aligned(residual, 16) ||
         !aligned(bias, 4))
         return fail(SDM_ERR_INVALID_ARG, "misaligned pointer (16-byte alignment required)");
     const int rc = check_ws(workspace, ws_bytes, sdm_linear_workspace_bytes(x_dtype, w_dtype, B, T, K, N));
@@ -136,6 +138,7 @@ int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dty
     g.combos = combos_of(w_dtype);
     g.out = lin_tokens(y, y_dtype, B, T, N, y_heads);
     g.pre = z;
+    g.rest = z_rest;
     g.bias = bias;
     g.residual = residual;
     g.act = act;
@@ -171,8 +174,8 @@ size_t sdm_linear_bwd_workspace_bytes(int x_dtype, int w_dtype, int act, int dy_
     return bwd_ws(x_dtype, w_dtype, act, dy_dtype, y_heads, B * T, K, N).total;
 }
 
-int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const void* z, int z_dtype,
-                   int act, const void* dy, int dy_dtype, int B, int T, int K, int N, int y_heads, void* dx, void* dw,
+int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const void* z,
+                   const void* z_rest, int z_dtype, int act, const void* dy, int dy_dtype, int B, int T, int K, int N, int y_heads, void* dx, void* dw,
                    float* dbias, void* workspace, size_t ws_bytes, void* stream) {
     sdm_set_error(SDM_OK, "");
     if (const char* m = bad_sizes(x_dtype, x_heads, w_dtype, act, B, T, K, N, y_heads))
@@ -182,11 +185,12 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         return fail(SDM_ERR_INVALID_ARG, "dtypes must be SDM_F32 or SDM_BF16");
     if (w_dtype == SDM_F32 && (dy_dtype != SDM_F32 || (act && z_dtype != SDM_F32)))
         return fail(SDM_ERR_INVALID_ARG, "an fp32 w needs fp32 z and dy");
+    if (act && z_rest && z_dtype != SDM_BF16) return fail(SDM_ERR_INVALID_ARG, "z_rest goes with a bf16 z");
     if (act && !z && (int64_t)B * T > 0) return fail(SDM_ERR_INVALID_ARG, "an activation's gradient needs z");
     if (!dx && !dw && !dbias) return SDM_OK;
     const int M = B * T;
     if (M > 0 && (!x || !w || !dy)) return fail(SDM_ERR_INVALID_ARG, "null pointer");
-    if (!aligned(x, 16) || !aligned(w, 16) || !aligned(z, 16) || !aligned(dy, 16) || !aligned(dx, 16) ||
+    if (!aligned(x, 16) || !aligned(w, 16) || !aligned(z, 16) || !aligned(z_rest, 16) || !aligned(dy, 16) || !aligned(dx, 16) ||
         !aligned(dw, 16) || !aligned(dbias, 4))
         return fail(SDM_ERR_INVALID_ARG, "misaligned pointer (16-byte alignment required)");
     hipStream_t st = (hipStream_t)stream;
@@ -203,7 +207,7 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
     const int np = parts_of(w_dtype);
     SdmProfScope ps(SDM_K_LINEAR, st);
     if (!L.direct || dbias)
-        e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_dtype, act, np, up64(M), up64(N),
+        e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_rest, z_dtype, act, np, up64(M), up64(N),
                                  L.direct ? nullptr : ws + L.dz, reinterpret_cast<float*>(ws + L.parts), dbias, st);
     LinGemm g{};
     g.combos = combos_of(w_dtype);

@@ -82,8 +82,8 @@ def lib() -> ctypes.CDLL:
         L.sdm_gdn_saved_bytes.argtypes = [I, I, I, I, I]
         for f in ("sdm_gdn_fwd_workspace_bytes", "sdm_gdn_bwd_workspace_bytes", "sdm_gdn_saved_bytes"):
             getattr(L, f).restype = SZ
-        L.sdm_linear.argtypes = [P, I, I, P, I, P, I, P, I, I, I, I, I, P, I, P, P, SZ, P]
-        L.sdm_linear_bwd.argtypes = [P, I, I, P, I, P, I, I, P, I, I, I, I, I, I, P, P, P, P, SZ, P]
+        L.sdm_linear.argtypes = [P, I, I, P, I, P, I, P, I, I, I, I, I, P, I, P, P, P, SZ, P]
+        L.sdm_linear_bwd.argtypes = [P, I, I, P, I, P, P, I, I, P, I, I, I, I, I, I, P, P, P, P, SZ, P]
         L.sdm_linear_workspace_bytes.argtypes = [I, I, I, I, I, I]
         L.sdm_linear_bwd_workspace_bytes.argtypes = [I, I, I, I, I, I, I, I, I]
         L.sdm_linear_workspace_bytes.restype = SZ
@@ -742,11 +742,12 @@ def linear_workspace(x, w) -> torch.Tensor:
 
 
 def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dtype=None, want_z: bool = False,
-           workspace=None, y=None):
+           want_rest: bool = False, workspace=None, y=None):
     """A projection: z = x w^T + bias, y = act(z) + residual (act 0 identity, 1 SiLU, 2 GELU).  x [B,T,K] or
     head-major [B,heads,T,d] (K = heads d); w [N,K]; bias [N] fp32; residual [B,T,N] in y's dtype.  Returns y
     [B,T,N], or head-major [B,heads,T,N/heads] where heads > 0, in out_dtype (w's by default, or float32), and
-    z (laid out and typed as y) if wanted.  An fp32 x with a bf16 w is rounded to bf16."""
+    z (laid out and typed as y) if wanted, and what a bf16 z's rounding left if that is wanted too (None of an
+    fp32 one).  An fp32 x with a bf16 w is rounded to bf16."""
     B, T, K, N, x_heads = _check_linear(x, w)
     heads = int(heads)
     if heads < 0 or (heads and N % heads):
@@ -769,21 +770,22 @@ def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dty
     if y is None:
         y = torch.empty(shape, dtype=dt, device=dev)
     z = torch.empty_like(y) if want_z else None
+    rest = torch.empty_like(y) if want_rest and want_z and dt == torch.bfloat16 else None
     if workspace is None and need:
         workspace = _ws(need, dev)
     with _current(dev):
         rc = lib().sdm_linear(_ptr(x), _dtype_code(x), x_heads, _ptr(w), _dtype_code(w), _ptr(bias), int(act),
-                              _ptr(residual), B, T, K, N, heads, _ptr(y), _dtype_code(y), _ptr(z), _ptr(workspace),
+                              _ptr(residual), B, T, K, N, heads, _ptr(y), _dtype_code(y), _ptr(z), _ptr(rest), _ptr(workspace),
                               0 if workspace is None else workspace.numel(), _stream(dev))
     _check("sdm_linear", rc)
-    return (y, z) if want_z else y
+    return (y, z, rest) if want_z and want_rest else (y, z) if want_z else y
 
 
-def linear_bwd(x, w, dy, z=None, act: int = 0, want_dx: bool = True, want_dw: bool = True, want_dbias: bool = False,
+def linear_bwd(x, w, dy, z=None, act: int = 0, z_rest=None, want_dx: bool = True, want_dw: bool = True, want_dbias: bool = False,
                workspace=None):
     """Reverse mode of linear: dz = dy act'(z), dx = dz w, dw = dz^T x, dbias = sum dz (residual's gradient is
-    dy).  dy [B,T,N] or head-major [B,heads,T,N/heads], in w's dtype or float32; z as linear returned it (not
-    needed with act 0).  Returns a dict of dx (as x), dw (as w) and dbias (fp32); None where not wanted."""
+    dy).  dy [B,T,N] or head-major [B,heads,T,N/heads], in w's dtype or float32; z (and z_rest) as linear
+    returned them (not needed with act 0; without z_rest the slope is taken at the rounded z).  Returns a dict of dx (as x), dw (as w) and dbias (fp32); None where not wanted."""
     B, T, K, N, x_heads = _check_linear(x, w)
     dB, dT, dN, heads = _tokens_of(dy, "dy")
     if (dB, dT, dN) != (B, T, N):
@@ -794,16 +796,21 @@ def linear_bwd(x, w, dy, z=None, act: int = 0, want_dx: bool = True, want_dw: bo
         raise ValueError("z is required for an activation's gradient")
     if z is not None:
         _expect(z, "z", tuple(dy.shape), (w.dtype, torch.float32))
+    if z_rest is not None:
+        if z is None:
+            raise ValueError("z_rest goes with z")
+        _expect(z_rest, "z_rest", tuple(dy.shape), (torch.bfloat16,))
+        _expect(z, "z", tuple(dy.shape), (torch.bfloat16,))
     codes = _dtype_code(x), _dtype_code(w), _dtype_code(dy)
     need = lib().sdm_linear_bwd_workspace_bytes(codes[0], codes[1], int(act), codes[2], B, T, K, N, heads)
     _check_ws(workspace, need)
-    dev = _dev(x, w, dy, z, workspace)
+    dev = _dev(x, w, dy, z, z_rest, workspace)
     out = dict(dx=torch.empty_like(x) if want_dx else None, dw=torch.empty_like(w) if want_dw else None,
                dbias=torch.empty((N,), dtype=torch.float32, device=dev) if want_dbias else None)
     if workspace is None:
         workspace = _ws(need, dev)
     with _current(dev):
-        rc = lib().sdm_linear_bwd(_ptr(x), codes[0], x_heads, _ptr(w), codes[1], _ptr(z),
+        rc = lib().sdm_linear_bwd(_ptr(x), codes[0], x_heads, _ptr(w), codes[1], _ptr(z), _ptr(z_rest),
                                   codes[1] if z is None else _dtype_code(z), int(act), _ptr(dy), codes[2], B, T, K, N,
                                   heads, _ptr(out["dx"]), _ptr(out["dw"]), _ptr(out["dbias"]), _ptr(workspace),
                                   workspace.numel(), _stream(dev))

@@ -108,6 +108,23 @@ def test_gradients(shape, kind, act):
     assert torch.equal(g3["dx"], g["dx"])
 
 
+@pytest.mark.parametrize("shape", [(3, 40, 64, 48, 0, 0), (2, 700, 40, 33, 0, 11), (1, 5, 64, 64, 4, 8)])
+def test_bias_gradient_at_the_unrounded_z(shape):
+    """With what z's rounding left, the slope is the fp32 one's to 2^-17 of z (|z act''| <= 1), and dbias an fp32 sum."""
+    B, T, K, N, hin, hout = shape
+    x, w, bias, _, dy = case(B, T, K, N, hin, hout, True)
+    for act in (1, 2):
+        y, z, rest = sdm.linear(x, w, bias, act=act, heads=hout, want_z=True, want_rest=True)
+        ry, rz = reference(x.double(), w.double(), bias.double(), act, None, hout)
+        close(z, rz, "z", BF16_TOL)
+        close(z.double() + rest.double(), rz, "z + rest", F32_TOL)
+        g = sdm.linear_bwd(x, w, dy, z=z, z_rest=rest, act=act, want_dbias=True)
+        zd = flat(rz).detach().requires_grad_()
+        dz, = torch.autograd.grad(ACTS[act](zd), zd, flat(dy.double()))
+        close(g["dbias"], dz.flatten(0, 1).sum(0), "dbias", F32_TOL)
+    assert sdm.linear(x.float(), w.float(), act=1, want_z=True, want_rest=True)[2] is None
+
+
 def test_gradients_against_differences():
     x, w, bias, _, dy = case(2, 20, 16, 12, 0, 3, False)
     for act in (1, 2):

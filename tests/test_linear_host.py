@@ -11,13 +11,13 @@ BIG = 1 << 40
 
 def fwd(**kw):
     a = dict(x=A, xd=1, xh=0, w=A, wd=1, bias=None, act=0, res=None, B=2, T=300, K=64, N=96, yh=0, y=A, yd=1, z=None,
-             ws=A, wsb=BIG)
+             rest=None, ws=A, wsb=BIG)
     a.update(kw)
     return L.sdm_linear(*a.values(), None)
 
 
 def bwd(**kw):
-    a = dict(x=A, xd=1, xh=0, w=A, wd=1, z=A, zd=1, act=1, dy=A, dyd=1, B=2, T=300, K=64, N=96, yh=0, dx=A, dw=A,
+    a = dict(x=A, xd=1, xh=0, w=A, wd=1, z=A, rest=None, zd=1, act=1, dy=A, dyd=1, B=2, T=300, K=64, N=96, yh=0, dx=A, dw=A,
              db=A, ws=A, wsb=BIG)
     a.update(kw)
     return L.sdm_linear_bwd(*a.values(), None)
@@ -31,7 +31,7 @@ SIZES = [(dict(B=-1), -1), (dict(T=-1), -1), (dict(K=0), -1), (dict(N=0), -1), (
 
 
 @pytest.mark.parametrize("kw,code", SIZES + [
-    (dict(y=None), -1), (dict(y=A + 8), -1), (dict(z=A + 4), -1), (dict(res=A + 2), -1), (dict(bias=A + 2), -1),
+    (dict(y=None), -1), (dict(y=A + 8), -1), (dict(z=A + 4), -1), (dict(res=A + 2), -1), (dict(rest=A), -1), (dict(z=A, rest=A + 4), -1), (dict(z=A, rest=A, yd=0), -1), (dict(bias=A + 2), -1),
     (dict(yd=2), -1), (dict(xd=0, wd=0, yd=1), -1), (dict(res=A, yh=8), -1),
     (dict(xd=0, wd=0, yd=0, ws=None), -1), (dict(xd=0, wd=0, yd=0, wsb=16), -3)])
 def test_forward_refuses(kw, code):
@@ -41,7 +41,7 @@ def test_forward_refuses(kw, code):
 
 @pytest.mark.parametrize("kw,code", SIZES + [
     (dict(z=None), -1), (dict(dy=None), -1), (dict(dy=A + 8), -1), (dict(dx=A + 8), -1), (dict(dw=A + 8), -1),
-    (dict(db=A + 2), -1), (dict(zd=3), -1), (dict(dyd=3), -1), (dict(xd=0, wd=0, dyd=1, zd=0), -1),
+    (dict(db=A + 2), -1), (dict(zd=3), -1), (dict(dyd=3), -1), (dict(rest=A, zd=0), -1), (dict(rest=A + 8), -1), (dict(xd=0, wd=0, dyd=1, zd=0), -1),
     (dict(xd=0, wd=0, dyd=0, zd=1), -1), (dict(ws=None), -1), (dict(wsb=100), -3), (dict(ws=A + 64), -1)])
 def test_backward_refuses(kw, code):
     assert bwd(**kw) == code
@@ -72,7 +72,8 @@ def test_binding_refuses(kw):
 
 @pytest.mark.parametrize("kw", [
     dict(dy=_t(2, 5, 16)), dict(dy=_t(2, 6, 12)), dict(dy=_t(2, 5, 12).double()), dict(act=1),
-    dict(act=1, z=_t(2, 3, 5, 4)), dict(z=_t(2, 5, 12).double()), dict(workspace=torch.zeros(1, dtype=torch.uint8))])
+    dict(act=1, z=_t(2, 3, 5, 4)), dict(z=_t(2, 5, 12).double()), dict(z_rest=_t(2, 5, 12, dt=torch.bfloat16)),
+    dict(z=_t(2, 5, 12), z_rest=_t(2, 5, 12, dt=torch.bfloat16)), dict(workspace=torch.zeros(1, dtype=torch.uint8))])
 def test_binding_refuses_backward(kw):
     a = dict(x=_t(2, 5, 16), w=_t(12, 16), dy=_t(2, 5, 12))
     a.update(kw)
