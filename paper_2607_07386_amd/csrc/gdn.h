@@ -200,13 +200,6 @@ struct GdnIn<bf16_t> {
 };
 
 // ---- staging of fragments: memory -> registers (a chunk ahead) -> LDS ----
-// N fragments of this wave, `first` on, from fragments as the prep kernel laid
-// them out; a fragment is 1 KB, 16 bytes a lane.
-template <int N>
-GDN_DEV void gdn_fetch(u4v (&r)[N], const uint16_t* base, int first) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u4v*>(base + (size_t)(first + i) * GDN_FRAG + lane_id() * 8);
-}
 // Buffers of one chunk or one state: a load past `bytes` gives zeros and a store there
 // does nothing, so rows past a sequence's end and past d_k need no branch (a branch
 // around a store makes the compiler wait for every load in flight at the next use).
@@ -236,25 +229,52 @@ GDN_DEV void gdn_ld8(__amdgpu_buffer_rsrc_t r, uint32_t off, int p, int n, float
         x[4 + i] = b[i];
     }
 }
-// Fragments first .. first + N - 1 of the [4][KTN] of 64 rows of a bf16 matrix of `rows` rows of
-// n values (n % 4 == 0): fragment (m, kb), lane row gdn_row(m, lane & 15).  Rows and depths past
-// the end are zero.
-template <int KTN, int N>
-GDN_DEV void gdn_fetch_rows(u4v (&r)[N], const bf16_t* base, int first, int rows, int n) {
-    const auto buf = gdn_buf(base, (size_t)min(rows, GDN_C) * n * 2);
+// Fragments first .. first + N - 1 of the [4][KTN] of 64 rows of a matrix of `rows` rows of n
+// values (n % 4 == 0): fragment (m, kb), lane row gdn_row(m, lane & 15).  Rows and depths past
+// the end are zero.  fp32 values are fetched as they are and cut into parts when staged.
+template <typename VT, int N>
+struct GdnAhead;
+template <int N>
+struct GdnAhead<bf16_t, N> {
+    u4v r[N];
+    template <int KTN>
+    GDN_DEV void fetch(const bf16_t* base, int first, int rows, int n) {
+        const auto buf = gdn_buf(base, (size_t)min(rows, GDN_C) * n * 2);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int m = (first + i) / KTN, p = 32 * ((first + i) % KTN) + 8 * (lane_id() >> 4);
-        const uint32_t o = (uint32_t)(gdn_row(m, lane_id() & 15) * n + p) * 2;
-        if (n % 8 == 0) {
-            r[i] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(buf, (int)(p < n ? o : GDN_OUT), 0, 0));
-        } else {
-            const u2v lo = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p < n ? o : GDN_OUT), 0, 0));
-            const u2v hi = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p + 4 < n ? o + 8 : GDN_OUT), 0, 0));
-            r[i] = u4v{lo.x, lo.y, hi.x, hi.y};
+        for (int i = 0; i < N; ++i) {
+            const int m = (first + i) / KTN, p = 32 * ((first + i) % KTN) + 8 * (lane_id() >> 4);
+            const uint32_t o = (uint32_t)(gdn_row(m, lane_id() & 15) * n + p) * 2;
+            if (n % 8 == 0) {
+                r[i] = __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(buf, (int)(p < n ? o : GDN_OUT), 0, 0));
+            } else {
+                const u2v lo = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p < n ? o : GDN_OUT), 0, 0));
+                const u2v hi = __builtin_bit_cast(u2v, __builtin_amdgcn_raw_buffer_load_b64(buf, (int)(p + 4 < n ? o + 8 : GDN_OUT), 0, 0));
+                r[i] = u4v{lo.x, lo.y, hi.x, hi.y};
+            }
         }
     }
-}
+    GDN_DEV void stage(uint16_t* lds, int first) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u4v*>(lds + (first + i) * GDN_FRAG + lane_id() * 8) = r[i];
+    }
+};
+template <int N>
+struct GdnAhead<float, N> {
+    float r[N][8];
+    template <int KTN>
+    GDN_DEV void fetch(const float* base, int first, int rows, int n) {
+        const auto buf = gdn_buf(base, (size_t)min(rows, GDN_C) * n * 4);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int m = (first + i) / KTN, p = 32 * ((first + i) % KTN) + 8 * (lane_id() >> 4);
+            gdn_ld8(buf, (uint32_t)(gdn_row(m, lane_id() & 15) * n + p) * 4, p, n, r[i]);
+        }
+    }
+    GDN_DEV void stage(uint16_t* lds, int first) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) gdn_store_frag<3>(lds, first + i, gdn_split(r[i]));
+    }
+};
 // Tiles d0 .. d0 + N - 1 of a state's 16 columns at the lane's column offset `co` (bytes), in the C layout.
 template <int N>
 GDN_DEV void gdn_load_state(sdm_f32x4 (&S)[N], const float* p, int d0, int dk, int dv, uint32_t co) {
@@ -272,12 +292,6 @@ GDN_DEV void gdn_store_state(const sdm_f32x4 (&S)[N], float* p, int d0, int dk, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) gdn_stf(buf, gdn_row(d0 + d, 4 * (lane_id() >> 4) + r) * dv * 4 + co, S[d][r]);
 }
-template <int N>
-GDN_DEV void gdn_stage(uint16_t* lds, int first, const u4v (&r)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) *reinterpret_cast<u4v*>(lds + (first + i) * GDN_FRAG + lane_id() * 8) = r[i];
-}
-
 // Fragments `wave`, `wave` + NW, ... of the n laid out at base (past the end: the last one again).
 template <int NW, int N>
 GDN_DEV void gdn_fetch_turns(u4v (&r)[N], const uint16_t* base, int n, int wave) {
@@ -294,21 +308,24 @@ GDN_DEV void gdn_stage_turns(uint16_t* lds, int n, int wave, const u4v (&r)[N]) 
 // Rows gdn_row(dt, .) of the transpose of a matrix that stands in LDS as the fragments
 // [4][KTN] of its 64 rows, depths 32 kb .. 32 kb + 31 (its rows): the transposing read takes
 // four rows of four columns from four lanes each, wherever they are.
-template <int KTN>
-GDN_DEV GdnFrag<1> gdn_turned_frag(const uint16_t* lds, int dt, int kb) {
+template <int KTN, int NT = 1>
+GDN_DEV GdnFrag<NT> gdn_turned_frag(const uint16_t* lds, int dt, int kb) {
     typedef short s4 __attribute__((ext_vector_type(4)));
     const int l = lane_id(), row = 4 * (l >> 4) + ((l & 15) >> 2);   // row of the source tile
-    union {
-        s4 s[2];
-        sdm_bf16x8 v;
-    } f;
+    GdnFrag<NT> r;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint16_t* p = lds + ((2 * kb + h) * KTN + (dt >> 1)) * GDN_FRAG + ((l & 3) * 16 + row) * 8 + (dt & 1) * 4;
-        f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p);
+    for (int x = 0; x < NT; ++x) {
+        union {
+            s4 s[2];
+            sdm_bf16x8 v;
+        } f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint16_t* p = lds + (((2 * kb + h) * KTN + (dt >> 1)) * NT + x) * GDN_FRAG + ((l & 3) * 16 + row) * 8 + (dt & 1) * 4;
+            f.s[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)p);
+        }
+        r.t[x] = f.v;
     }
-    GdnFrag<1> r;
-    r.t[0] = f.v;
     return r;
 }
 

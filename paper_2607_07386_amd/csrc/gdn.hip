@@ -321,8 +321,8 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
         for (int r = 0; r < 4; ++r) M[(16 * w + 4 * g + r) * LD + 16 * j + r16] = qk[j][r];
     __syncthreads();
     blocks(a.pf);
-    // fp32: K^T (and Q^T) of the key head, rows of d_k, depth = tokens (bf16 scans turn K in LDS)
-    if constexpr (NT == 3) {
+    // fp32: K^T and Q^T of the key head, rows of d_k, depth = tokens, for the kernels that do not turn K in LDS
+    if constexpr (NT == 3 && (BWD || KTN == 8)) {
         if (h % G) return;
         const size_t ck = (size_t)(b * a.Hk + hk) * a.nC + c;
         for (int f = w; f < (BWD ? 2 : 1) * DT * 2; f += 4) {
@@ -341,13 +341,14 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
 }
 
 // ---------------------------------------------------------------- scan
-// fp32 inputs: one wave per 16 columns of a stream's state, four to a workgroup; the waves
+// fp32 inputs with d_k > 128, whose chunk LDS does not hold: one wave per 16 columns, four to a
+// workgroup; the waves
 // share nothing (each reads the chunk's fragments itself) and never wait for
 // one another.  The state stays in the C layout of its own update.
-template <int KTN, bool SAVE>
-__global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
+template <bool SAVE>
+__global__ __launch_bounds__(256, 1) void gdn_scan_wide_kernel(GdnArgs a) {
     using VT = float;
-    constexpr int NT = 3, DT = 2 * KTN;
+    constexpr int NT = 3, KTN = 8, DT = 2 * KTN;
     const int groups = (a.dv + 63) / 64;
     int grp, bh;
     scan_wg_coords<true>(groups, grp, bh);
@@ -470,35 +471,36 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_kernel(GdnArgs a) {
         }
 }
 
-// The same walk for bf16 inputs, two waves to 16 columns: half h holds tokens 32 h .. + 31 of the
+// Two waves to 16 columns: half h holds tokens 32 h .. + 31 of the
 // chunk and one half of the state's rows, so that a chunk's chain of dependent products
 // is half as long and twice as many waves share the device.  What a half needs of the
 // other (the state's fragments, R and E of the first 32 tokens, E for the update)
 // passes through LDS.  The chunk's K, Q, T' and P are fetched into registers a chunk
 // ahead and staged once for the workgroup; K^T is K read with the transposing loads.
-template <int KTN, int NCT_>
+template <typename VT, int KTN, int NCT_>
 struct ScanCfg {
+    static constexpr int NT = GdnIn<VT>::NT;
     static constexpr int NCT = NCT_;                   // column tiles of a workgroup
     static constexpr int NW = 2 * NCT;
-    static constexpr bool QD = KTN == 8;               // Q straight from memory: LDS is full
+    static constexpr bool QD = NT == 1 ? KTN == 8 : KTN == 4;   // Q straight from memory: LDS is full
     static constexpr int FPW = 4 * KTN / NW;           // fragments of K (and Q) that a wave moves
     static constexpr int TPW = (18 + NW - 1) / NW;     // of T' (and P)
     static constexpr int XCH = (KTN + 3) * 3;          // exchanged fragments per column tile: S, then E_a, E'_a, E'_b (R_a)
     static constexpr size_t LDS =
-        (size_t)(4 * KTN * (QD ? 1 : 2) + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+        (size_t)(4 * KTN * NT * (QD ? 1 : 2) + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
 };
 
-template <int KTN, int NCT, bool SAVE>
+template <typename VT, int KTN, int NCT, bool SAVE>
 __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a) {
-    using C = ScanCfg<KTN, NCT>;
-    constexpr int NW = C::NW, KH = KTN / 2;            // KH: 32-row blocks of the state per wave
+    using C = ScanCfg<VT, KTN, NCT>;
+    constexpr int NT = C::NT, NW = C::NW, KH = KTN / 2;            // KH: 32-row blocks of the state per wave
     extern __shared__ __align__(16) unsigned char smem[];
-    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN]
-    uint16_t* sT = sK + 4 * KTN * GDN_FRAG;                 // T' [6][3]
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN][NT]
+    uint16_t* sT = sK + 4 * KTN * NT * GDN_FRAG;                 // T' [6][3]
     uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;
     uint16_t* sX = sP + GDN_BLKS * 3 * GDN_FRAG;            // exchange, per column tile
     float* sV = reinterpret_cast<float*>(sX + C::NCT * C::XCH * GDN_FRAG);   // [2][gamma, end, beta][64]
-    uint16_t* sQ = reinterpret_cast<uint16_t*>(sV + 2 * 3 * 64);             // [4][KTN] unless QD
+    uint16_t* sQ = reinterpret_cast<uint16_t*>(sV + 2 * 3 * 64);             // [4][KTN][NT] unless QD
 
     const int groups = (a.dv + 16 * C::NCT - 1) / (16 * C::NCT);
     int grp, bh;
@@ -509,15 +511,15 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
     const int ct = w % C::NCT, h = w / C::NCT;
     const int col = (grp * C::NCT + ct) * 16 + r16;
     const bool cv = col < a.dv;
-    const uint32_t co = cv ? col * 4 : GDN_OUT, co2 = cv ? col * 2 : GDN_OUT;   // column offsets: fp32, bf16
+    const uint32_t co = cv ? col * 4 : GDN_OUT, cov = cv ? col * sizeof(VT) : GDN_OUT;   // column offsets: fp32, v's type
     const size_t sn = (size_t)a.dk * a.dv;
     const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
     uint16_t* xS = sX + ct * C::XCH * GDN_FRAG;             // [KTN][3]
     uint16_t *xE = xS + KTN * 3 * GDN_FRAG, *xA = xE + 3 * GDN_FRAG, *xB = xA + 3 * GDN_FRAG;   // xB: R_a until E'_b
 
-    const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
-    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
-    const bf16_t* vp = static_cast<const bf16_t*>(a.v) + (size_t)bh * a.T * a.dv;
+    const VT* kp = static_cast<const VT*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const VT* qp = static_cast<const VT*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const VT* vp = static_cast<const VT*>(a.v) + (size_t)bh * a.T * a.dv;
     const size_t ch0 = (size_t)bh * a.nC;
 
     sdm_f32x4 S[KTN];                                       // this half's tiles
@@ -531,28 +533,29 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
         }
     };
 
-    u4v rK[C::FPW], rQ[C::FPW], rT[C::TPW], rP[C::TPW];
+    GdnAhead<VT, C::FPW> rK, rQ;
+    u4v rT[C::TPW], rP[C::TPW];
     float rV, rB = 0.f, V[2][4];                            // rB: beta where the workgroup has two waves
-    const auto fetch_k = [&](int c) { gdn_fetch_rows<KTN>(rK, kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk); };
+    const auto fetch_k = [&](int c) { rK.template fetch<KTN>(kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk); };
     const auto fetch_q = [&](int c) {
-        if constexpr (!C::QD) gdn_fetch_rows<KTN>(rQ, qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        if constexpr (!C::QD) rQ.template fetch<KTN>(qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
         const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // waves 3 on repeat wave 2
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
         if constexpr (NW == 2) rB = a.vec[(ch0 + c) * GDN_VEC * 64 + GDN_V_BETA * 64 + lane];
     };
     const auto fetch_v = [&](int c) {
         const int t0 = c * GDN_C;
-        const auto buf = gdn_buf(vp + (size_t)t0 * a.dv, (size_t)min(len - t0, GDN_C) * a.dv * 2);
+        const auto buf = gdn_buf(vp + (size_t)t0 * a.dv, (size_t)min(len - t0, GDN_C) * a.dv * sizeof(VT));
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) V[m][r] = gdn_ld1<bf16_t>(buf, gdn_row(2 * h + m, 4 * g + r) * a.dv * 2 + co2);
+            for (int r = 0; r < 4; ++r) V[m][r] = gdn_ld1<VT>(buf, gdn_row(2 * h + m, 4 * g + r) * a.dv * sizeof(VT) + cov);
     };
     const auto fetch_t = [&](int c) { gdn_fetch_turns<NW>(rT, a.tf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
     const auto fetch_p = [&](int c) { gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
-    const auto stage_k = [&]() { gdn_stage(sK, w * C::FPW, rK); };
+    const auto stage_k = [&]() { rK.stage(sK, w * C::FPW); };
     const auto stage_q = [&](int par) {
-        if constexpr (!C::QD) gdn_stage(sQ, w * C::FPW, rQ);
+        if constexpr (!C::QD) rQ.stage(sQ, w * C::FPW);
         if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
         if (NW == 2 && w == 0) sV[(par * 3 + 2) * 64 + lane] = rB;
     };
@@ -590,14 +593,14 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
         for (int m = 0; m < 2; ++m) R[m] = Y[m] = X[m] = zero;
         const auto rows_by_state = [&](int kb, const GdnFrag<3>& s) {
 #pragma unroll
-            for (int m = 0; m < 2; ++m) R[m] = gdn_mm(gdn_load_frag<1>(sK, (2 * h + m) * KTN + kb), s, R[m]);
+            for (int m = 0; m < 2; ++m) R[m] = gdn_mm(gdn_load_frag<NT>(sK, (2 * h + m) * KTN + kb), s, R[m]);
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 if constexpr (C::QD) {
                     const int row = gdn_row(2 * h + m, r16);
-                    Y[m] = gdn_mm(gdn_row_frag<1>(qp + (size_t)(t0 + row) * a.dk, kb, a.dk, row < left), s, Y[m]);
+                    Y[m] = gdn_mm(gdn_row_frag<NT>(qp + (size_t)(t0 + row) * a.dk, kb, a.dk, row < left), s, Y[m]);
                 } else {
-                    Y[m] = gdn_mm(gdn_load_frag<1>(sQ, (2 * h + m) * KTN + kb), s, Y[m]);
+                    Y[m] = gdn_mm(gdn_load_frag<NT>(sQ, (2 * h + m) * KTN + kb), s, Y[m]);
                 }
             }
         };
@@ -657,8 +660,8 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
 #pragma unroll
             for (int d = 0; d < KTN; ++d) {
                 S[d] *= last;
-                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, h), uf, S[d]);
-                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, 1 - h), uo, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sK, h * KTN + d, h), uf, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sK, h * KTN + d, 1 - h), uo, S[d]);
             }
         }
         if (h == 1) {
@@ -683,10 +686,10 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
     gdn_store_state(S, a.stateT + bh * sn, h * KTN, a.dk, a.dv, co);
 }
 
-template <int KTN, int NCT, bool SAVE>
+template <typename VT, int KTN, int NCT, bool SAVE>
 hipError_t launch_scan_tiles(const GdnArgs& a, hipStream_t st) {
-    using C = ScanCfg<KTN, NCT>;
-    const auto kfn = gdn_scan_halves_kernel<KTN, NCT, SAVE>;
+    using C = ScanCfg<VT, KTN, NCT>;
+    const auto kfn = gdn_scan_halves_kernel<VT, KTN, NCT, SAVE>;
     hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
     if (e != hipSuccess) return e;
     kfn<<<dim3((a.dv + 16 * C::NCT - 1) / (16 * C::NCT) * a.B * a.H), C::NW * 64, C::LDS, st>>>(a);
@@ -695,13 +698,20 @@ hipError_t launch_scan_tiles(const GdnArgs& a, hipStream_t st) {
 
 // Column tiles to a workgroup: as many as leave a workgroup to every compute unit. More
 // share one staging of the chunk, but also one LDS, whose reads then set the pace.
-template <int KTN, bool SAVE>
-hipError_t launch_scan_halves(const GdnArgs& a, hipStream_t st) {
-    const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
-    if constexpr (KTN < 8) {
-        if (tiles >= 4 * cus) return launch_scan_tiles<KTN, 4, SAVE>(a, st);
+template <typename VT, int KTN, bool SAVE>
+hipError_t launch_scan(const GdnArgs& a, hipStream_t st) {
+    if constexpr (KTN == 8 && sizeof(VT) == 4) {
+        const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
+        gdn_scan_wide_kernel<SAVE><<<grid, 256, 0, st>>>(a);
+        return hipGetLastError();
+    } else {
+        constexpr int MOST = KTN == 2 ? 4 : KTN == 4 && sizeof(VT) == 2 ? 4 : 2;   // what LDS holds
+        const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
+        if constexpr (MOST == 4) {
+            if (tiles >= 4 * cus) return launch_scan_tiles<VT, KTN, 4, SAVE>(a, st);
+        }
+        return tiles >= 2 * cus ? launch_scan_tiles<VT, KTN, 2, SAVE>(a, st) : launch_scan_tiles<VT, KTN, 1, SAVE>(a, st);
     }
-    return tiles >= 2 * cus ? launch_scan_tiles<KTN, 2, SAVE>(a, st) : launch_scan_tiles<KTN, 1, SAVE>(a, st);
 }
 
 }  // namespace
@@ -768,16 +778,14 @@ hipError_t sdm_launch_gdn_prep(const GdnArgs& a, bool backward, hipStream_t st) 
 }
 
 hipError_t sdm_launch_gdn_scan(const GdnArgs& a, hipStream_t st) {
-    const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
     const bool bf = a.in_dtype == SDM_DT_BF16, save = a.saved_S != nullptr;
-#define K(N)                                                                                 \
-    do {                                                                                     \
-        if (bf && save) return launch_scan_halves<N, true>(a, st);                           \
-        else if (bf) return launch_scan_halves<N, false>(a, st);                             \
-        else if (save) gdn_scan_kernel<N, true><<<grid, 256, 0, st>>>(a);             \
-        else gdn_scan_kernel<N, false><<<grid, 256, 0, st>>>(a);                      \
+#define K(N)                                                       \
+    do {                                                           \
+        if (bf && save) return launch_scan<bf16_t, N, true>(a, st); \
+        if (bf) return launch_scan<bf16_t, N, false>(a, st);       \
+        if (save) return launch_scan<float, N, true>(a, st);       \
+        return launch_scan<float, N, false>(a, st);                \
     } while (0)
     GDN_PICK_KTN(K);
 #undef K
-    return hipGetLastError();
 }

@@ -22,11 +22,10 @@
 
 namespace {
 
-// fp32 inputs: one wave per 16 columns, as gdn_scan_kernel
-template <int KTN>
-__global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
+// fp32 inputs with d_k > 128: one wave per 16 columns, as gdn_scan_wide_kernel
+__global__ __launch_bounds__(256, 1) void gdn_adjoint_wide_kernel(GdnArgs a) {
     using VT = float;
-    constexpr int NT = 3, DT = 2 * KTN;
+    constexpr int NT = 3, KTN = 8, DT = 2 * KTN;
     const int groups = (a.dv + 63) / 64;
     int grp, bh;
     scan_wg_coords<true>(groups, grp, bh);
@@ -146,28 +145,29 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_kernel(GdnArgs a) {
     }
 }
 
-// The same walk for bf16 inputs, two waves to 16 columns as in the forward scan: half h
+// Two waves to 16 columns as in the forward scan: half h
 // holds tokens 32 h .. + 31 and one half of the state's rows.  dY is read whole by both
 // (its part below needs no exchange); F = diag(beta) dE of the last 32 tokens and -G dR
 // pass through LDS.
-template <int KTN, int NCT_>
+template <typename VT, int KTN, int NCT_>
 struct AdjCfg {
+    static constexpr int NT = GdnIn<VT>::NT;
     static constexpr int NCT = NCT_;
     static constexpr int NW = 2 * NCT;
     static constexpr int FPW = 4 * KTN / NW;
     static constexpr int TPW = (18 + NW - 1) / NW;
     static constexpr int XCH = (KTN + 3) * 3;          // S, then F_b, N_a, N_b
-    static constexpr size_t LDS = (size_t)(8 * KTN + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+    static constexpr size_t LDS = (size_t)(8 * KTN * NT + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
 };
 
-template <int KTN, int NCT>
+template <typename VT, int KTN, int NCT>
 __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArgs a) {
-    using C = AdjCfg<KTN, NCT>;
-    constexpr int NW = C::NW, KH = KTN / 2;
+    using C = AdjCfg<VT, KTN, NCT>;
+    constexpr int NT = C::NT, NW = C::NW, KH = KTN / 2;
     extern __shared__ __align__(16) unsigned char smem[];
-    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN]
-    uint16_t* sQ = sK + 4 * KTN * GDN_FRAG;
-    uint16_t* sT = sQ + 4 * KTN * GDN_FRAG;                 // T'^T [6][3]
+    uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN][NT]
+    uint16_t* sQ = sK + 4 * KTN * NT * GDN_FRAG;
+    uint16_t* sT = sQ + 4 * KTN * NT * GDN_FRAG;                 // T'^T [6][3]
     uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;            // P^T
     uint16_t* sX = sP + GDN_BLKS * 3 * GDN_FRAG;
     float* sV = reinterpret_cast<float*>(sX + C::NCT * C::XCH * GDN_FRAG);   // [2][gamma, end, beta][64]
@@ -186,8 +186,8 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
     uint16_t* xS = sX + ct * C::XCH * GDN_FRAG;             // [KTN][3]
     uint16_t *xF = xS + KTN * 3 * GDN_FRAG, *xA = xF + 3 * GDN_FRAG, *xB = xA + 3 * GDN_FRAG;
 
-    const bf16_t* kp = static_cast<const bf16_t*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
-    const bf16_t* qp = static_cast<const bf16_t*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const VT* kp = static_cast<const VT*>(a.k) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
+    const VT* qp = static_cast<const VT*>(a.q) + (size_t)(b * a.Hk + hk) * a.T * a.dk;
     const size_t ch0 = (size_t)bh * a.nC;
 
     sdm_f32x4 S[KTN];
@@ -201,11 +201,12 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
         }
     };
 
-    u4v rK[C::FPW], rQ[C::FPW], rT[C::TPW], rP[C::TPW];
+    GdnAhead<VT, C::FPW> rK, rQ;
+    u4v rT[C::TPW], rP[C::TPW];
     float rV, rY[4][4];
     const auto fetch_kq = [&](int c) {
-        gdn_fetch_rows<KTN>(rK, kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
-        gdn_fetch_rows<KTN>(rQ, qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        rK.template fetch<KTN>(kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        rQ.template fetch<KTN>(qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
         const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // other waves repeat beta
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
     };
@@ -221,8 +222,8 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
     const auto fetch_t = [&](int c) { gdn_fetch_turns<NW>(rT, a.tf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
     const auto fetch_p = [&](int c) { gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
     const auto stage_kq = [&](int par) {
-        gdn_stage(sK, w * C::FPW, rK);
-        gdn_stage(sQ, w * C::FPW, rQ);
+        rK.stage(sK, w * C::FPW);
+        rQ.stage(sQ, w * C::FPW);
         if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
         if (NW == 2 && w == 0) sV[(par * 3 + 2) * 64 + lane] = rB;
     };
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
             const int kb = i < KH ? h * KH + i : (1 - h) * KH + i - KH;
             const GdnFrag<3> s = i < KH ? sf[i < KH ? i : 0] : gdn_load_frag<3>(xS, kb);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<1>(sK, (2 * h + m) * KTN + kb), s, dE[m]);
+            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<NT>(sK, (2 * h + m) * KTN + kb), s, dE[m]);
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -330,10 +331,10 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
 #pragma unroll
             for (int d = 0; d < KTN; ++d) {
                 S[d] *= last;
-                S[d] = gdn_mm(gdn_turned_frag<KTN>(sQ, h * KTN + d, 0), y0, S[d]);
-                S[d] = gdn_mm(gdn_turned_frag<KTN>(sQ, h * KTN + d, 1), y1, S[d]);
-                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, h), nf, S[d]);
-                S[d] = gdn_mm(gdn_turned_frag<KTN>(sK, h * KTN + d, 1 - h), no, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sQ, h * KTN + d, 0), y0, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sQ, h * KTN + d, 1), y1, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sK, h * KTN + d, h), nf, S[d]);
+                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sK, h * KTN + d, 1 - h), no, S[d]);
             }
         }
         give_state();
@@ -345,24 +346,29 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
     if (a.dstate0) gdn_store_state(S, a.dstate0 + bh * sn, h * KTN, a.dk, a.dv, co);
 }
 
-template <int KTN, int NCT>
+template <typename VT, int KTN, int NCT>
 hipError_t launch_adjoint_tiles(const GdnArgs& a, hipStream_t st) {
-    using C = AdjCfg<KTN, NCT>;
-    const auto kfn = gdn_adjoint_halves_kernel<KTN, NCT>;
+    using C = AdjCfg<VT, KTN, NCT>;
+    const auto kfn = gdn_adjoint_halves_kernel<VT, KTN, NCT>;
     hipError_t e = hipFuncSetAttribute((const void*)kfn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)C::LDS);
     if (e != hipSuccess) return e;
     kfn<<<dim3((a.dv + 16 * C::NCT - 1) / (16 * C::NCT) * a.B * a.H), C::NW * 64, C::LDS, st>>>(a);
     return hipGetLastError();
 }
 // column tiles to a workgroup as in the forward scan
-template <int KTN>
-hipError_t launch_adjoint_halves(const GdnArgs& a, hipStream_t st) {
-    const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
-    if constexpr (KTN < 8) {
-        if (tiles >= 4 * cus) return launch_adjoint_tiles<KTN, 4>(a, st);
-        if (tiles >= 2 * cus) return launch_adjoint_tiles<KTN, 2>(a, st);
+template <typename VT, int KTN>
+hipError_t launch_adjoint(const GdnArgs& a, hipStream_t st) {
+    if constexpr (KTN == 8 && sizeof(VT) == 4) {
+        gdn_adjoint_wide_kernel<<<dim3((a.dv + 63) / 64 * a.B * a.H), 256, 0, st>>>(a);
+        return hipGetLastError();
+    } else {
+        const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
+        if constexpr (KTN == 2 || (KTN == 4 && sizeof(VT) == 2)) {
+            if (tiles >= 4 * cus) return launch_adjoint_tiles<VT, KTN, 4>(a, st);
+            if (tiles >= 2 * cus) return launch_adjoint_tiles<VT, KTN, 2>(a, st);
+        }
+        return launch_adjoint_tiles<VT, KTN, 1>(a, st);
     }
-    return launch_adjoint_tiles<KTN, 1>(a, st);
 }
 
 // ---------------------------------------------------------------- gradients
@@ -488,10 +494,10 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
         // fragments go to LDS, where they are turned), and P or N
         float pn[4][4];
         constexpr int FPW = KTN / 2;          // fragments of K and of Q that a wave moves
-        u4v rK[FPW], rQ[FPW];
+        GdnAhead<bf16_t, FPW> rK, rQ;
         if constexpr (NT == 1) {
-            gdn_fetch_rows<KTN>(rK, static_cast<const bf16_t*>(a.k) + tq * a.dk, wave * FPW, left, a.dk);
-            gdn_fetch_rows<KTN>(rQ, static_cast<const bf16_t*>(a.q) + tq * a.dk, wave * FPW, left, a.dk);
+            rK.template fetch<KTN>(static_cast<const bf16_t*>(a.k) + tq * a.dk, wave * FPW, left, a.dk);
+            rQ.template fetch<KTN>(static_cast<const bf16_t*>(a.q) + tq * a.dk, wave * FPW, left, a.dk);
         }
         {
             const auto bpn = gdn_buf((half == 0 ? a.pm : a.nm) + ch * 64 * 64, 64 * 64 * 4);
@@ -502,8 +508,8 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
                     pn[j][r] = gdn_ldf(bpn, (uint32_t)(gdn_row(w, 4 * g + r) * 64 + gdn_row(j, r16)) * 4);
         }
         if constexpr (NT == 1) {
-            gdn_stage(sK, wave * FPW, rK);
-            gdn_stage(sQ, wave * FPW, rQ);
+            rK.stage(sK, wave * FPW);
+            rQ.stage(sQ, wave * FPW);
             __syncthreads();
         }
         // K^T, Q^T: columns of tile d0 + d, depths 32 kb on
@@ -685,15 +691,9 @@ hipError_t launch_grads(const GdnArgs& a, hipStream_t st) {
     } while (0)
 
 hipError_t sdm_launch_gdn_adjoint(const GdnArgs& a, hipStream_t st) {
-    const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
-#define F(N)                                                                                 \
-    do {                                                                                     \
-        if (a.in_dtype == SDM_DT_BF16) return launch_adjoint_halves<N>(a, st);               \
-        else gdn_adjoint_kernel<N><<<grid, 256, 0, st>>>(a);                          \
-    } while (0)
+#define F(N) return a.in_dtype == SDM_DT_BF16 ? launch_adjoint<bf16_t, N>(a, st) : launch_adjoint<float, N>(a, st)
     GDN_PICK(F);
 #undef F
-    return hipGetLastError();
 }
 
 hipError_t sdm_launch_gdn_grads(const GdnArgs& a, hipStream_t st) {
