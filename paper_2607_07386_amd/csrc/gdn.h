@@ -58,10 +58,15 @@ struct GdnArgs {
     uint16_t *kt, *qt;             // fragments of K^T, Q^T: [B Hk nC][dk/16][2][NT]
     float *pm, *nm;                // P and N as [64][64] (backward)
     float* dS;                     // [B H nC][dk][dv] adjoints at the chunks' ends (backward)
+    // the forward scan in `segs` segments of `seg_len` chunks each (1: the whole sequence):
+    int segs, seg_len;
+    float* seg_z;                  // [segs - 1][B H][dk][dv] a segment's end from the zero state, then from its true start
+    float* seg_phi;                // [segs - 1][B H][dk][dk] what it multiplies its start by
 };
 
 struct GdnWs {
-    size_t vec, tf, pf, kt, qt, pm, nm, dS, total;
+    size_t vec, tf, pf, kt, qt, pm, nm, dS, seg_z, seg_phi, total;
+    int segs, seg_len;
 };
 GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool backward);
 hipError_t sdm_launch_gdn_step(const GdnArgs& a, hipStream_t st);

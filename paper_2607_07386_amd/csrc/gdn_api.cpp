@@ -94,6 +94,10 @@ void set_ws(GdnArgs& a, const GdnWs& w, void* workspace) {
     a.pm = reinterpret_cast<float*>(p + w.pm);
     a.nm = reinterpret_cast<float*>(p + w.nm);
     a.dS = reinterpret_cast<float*>(p + w.dS);
+    a.seg_z = reinterpret_cast<float*>(p + w.seg_z);
+    a.seg_phi = reinterpret_cast<float*>(p + w.seg_phi);
+    a.segs = w.segs;
+    a.seg_len = w.seg_len;
 }
 
 size_t saved_states(int B, int H, int T, int d_k, int d_v) {

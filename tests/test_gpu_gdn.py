@@ -81,6 +81,49 @@ def test_long_memory_many_chunks():
     close(S, rS, "state")
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("dk,dv", [(16, 20), (128, 48)])
+def test_few_streams_in_segments(dk, dv, bf16):
+    """Long sequences of few streams run segments side by side: a full one, one that ends inside a segment,
+    one that ends inside the first, one empty; with the states for a backward too."""
+    T = 5 * 16 * 64 + 700
+    a, s0, _, _ = inputs(4, 1, 1, T, dk, dv, bf16, long_memory=True)
+    lens = torch.tensor([T, 3333, 50, 0], dtype=torch.int32, device=DEV)
+    on = (torch.arange(T, device=DEV)[None] < lens[:, None])[:, None, :, None]
+    ry, rS = definition(a, s0, lens)
+    y, S = sdm.gdn_fwd(**a, state0=s0, lens=lens)
+    close(torch.where(on, y, 0.0), ry, "y")
+    close(S, rS, "state")
+    saved = sdm.gdn_saved_buffer(4, 1, T, dk, dv, torch.device(DEV))
+    y2, S2 = sdm.gdn_fwd(**a, state0=s0, lens=lens, saved=saved)
+    assert torch.equal(y, y2) and torch.equal(S, S2)
+    mine = s0.clone()
+    sdm.gdn_fwd(**a, state0=mine, state_out=mine, lens=lens)
+    assert torch.equal(S, mine)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("B,H,dk,dv", [(16, 32, 32, 32), (16, 16, 64, 32), (32, 16, 100, 32), (16, 16, 128, 36),
+                                       (16, 16, 256, 32)])
+def test_many_streams(B, H, dk, dv, bf16):
+    """Enough column tiles for several to a workgroup, forward and backward."""
+    T = 70
+    a, s0, dy, dS = inputs(B, H // 2, H, T, dk, dv, bf16)
+    saved = sdm.gdn_saved_buffer(B, H, T, dk, dv, torch.device(DEV))
+    y, S = sdm.gdn_fwd(**a, state0=s0, saved=saved)
+    y2, S2 = sdm.gdn_fwd(**a, state0=s0)
+    assert torch.equal(y, y2) and torch.equal(S, S2)
+    leaves = {x: t.double().requires_grad_() for x, t in a.items()}
+    ls0 = s0.double().requires_grad_()
+    ry, rS = definition(leaves, ls0)
+    ref = torch.autograd.grad((ry, rS), [*leaves.values(), ls0], (dy.double(), dS.double()))
+    close(y, ry, "y")
+    close(S, rS, "state")
+    g = sdm.gdn_bwd(**a, saved=saved, dy=dy, dstate_T=dS)
+    for name, r in zip(("dq", "dk", "dv", "dalpha", "dbeta", "dstate0"), ref):
+        close(g[name], r, name)
+
+
 def test_empty_and_in_place():
     a, s0, _, _ = inputs(2, 1, 2, 0, 8, 12)
     y, S = sdm.gdn_fwd(**a, state0=s0)
