@@ -56,7 +56,6 @@ struct GdnArgs {
     float* vec;                    // [B H nC][GDN_VEC][64]
     uint16_t *tf, *pf;             // fragments of T' and P (forward), of their transposes (backward)
     uint16_t *kt, *qt;             // fragments of K^T, Q^T: [B Hk nC][dk/16][2][NT]
-    float *pm, *nm;                // P and N as [64][64] (backward)
     float* dS;                     // [B H nC][dk][dv] adjoints at the chunks' ends (backward)
     // the forward scan in `segs` segments of `seg_len` chunks each (1: the whole sequence):
     int segs, seg_len;
@@ -65,7 +64,7 @@ struct GdnArgs {
 };
 
 struct GdnWs {
-    size_t vec, tf, pf, kt, qt, pm, nm, dS, seg_z, seg_phi, total;
+    size_t vec, tf, pf, kt, qt, dS, seg_z, seg_phi, total;
     int segs, seg_len;
 };
 GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool backward);

@@ -244,10 +244,6 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
             }
             M[i * LD + cj] = n * bj;
             qk[j][r] = p;
-            if constexpr (BWD) {
-                a.pm[(ch * 64 + i) * 64 + cj] = p;
-                a.nm[(ch * 64 + i) * 64 + cj] = n;
-            }
         }
     }
     __syncthreads();
@@ -828,8 +824,6 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
     w.kt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
     if (backward) {
         w.qt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
-        w.pm = take(n * 64 * 64 * 4);
-        w.nm = take(n * 64 * 64 * 4);
         w.dS = take(n * dk * dv * 4);
     }
     w.total = o;

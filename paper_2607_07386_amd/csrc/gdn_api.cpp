@@ -91,8 +91,6 @@ void set_ws(GdnArgs& a, const GdnWs& w, void* workspace) {
     a.pf = reinterpret_cast<uint16_t*>(p + w.pf);
     a.kt = reinterpret_cast<uint16_t*>(p + w.kt);
     a.qt = reinterpret_cast<uint16_t*>(p + w.qt);
-    a.pm = reinterpret_cast<float*>(p + w.pm);
-    a.nm = reinterpret_cast<float*>(p + w.nm);
     a.dS = reinterpret_cast<float*>(p + w.dS);
     a.seg_z = reinterpret_cast<float*>(p + w.seg_z);
     a.seg_phi = reinterpret_cast<float*>(p + w.seg_phi);

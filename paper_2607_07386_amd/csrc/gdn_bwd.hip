@@ -490,22 +490,12 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
         __builtin_amdgcn_sched_barrier(0);
         through = wave_sum(through);
         if (lane == 0) rThr[wave] = through;
-        // everything the rest reads from memory, in one batch: K and Q of a bf16 input (their
-        // fragments go to LDS, where they are turned), and P or N
-        float pn[4][4];
+        // K and Q of a bf16 input: their fragments go to LDS, where they are turned
         constexpr int FPW = KTN / 2;          // fragments of K and of Q that a wave moves
         GdnAhead<bf16_t, FPW> rK, rQ;
         if constexpr (NT == 1) {
             rK.template fetch<KTN>(static_cast<const bf16_t*>(a.k) + tq * a.dk, wave * FPW, left, a.dk);
             rQ.template fetch<KTN>(static_cast<const bf16_t*>(a.q) + tq * a.dk, wave * FPW, left, a.dk);
-        }
-        {
-            const auto bpn = gdn_buf((half == 0 ? a.pm : a.nm) + ch * 64 * 64, 64 * 64 * 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    pn[j][r] = gdn_ldf(bpn, (uint32_t)(gdn_row(w, 4 * g + r) * 64 + gdn_row(j, r16)) * 4);
         }
         if constexpr (NT == 1) {
             rK.stage(sK, wave * FPW);
@@ -521,6 +511,28 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
             if constexpr (NT == 1) return gdn_turned_frag<KTN>(sQ, d0 + d, kb);
             else return gdn_load_frag<3>(a.qt, (ck * DT + d0 + d) * 2 + kb);
         };
+        // Q K^T (first half's waves) or K K^T of the wave's rows: P and N but for the decays
+        sdm_f32x4 pn[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) pn[j] = zero;
+#pragma unroll
+        for (int kb = 0; kb < KTN; ++kb) {
+            GdnFrag<NT> fa;
+            if constexpr (NT == 1) fa = gdn_load_frag<1>(half == 0 ? sQ : sK, w * KTN + kb);
+            else fa = gdn_row_frag<NT>(static_cast<const VT*>(half == 0 ? a.q : a.k) + (tq + arow) * a.dk, kb, a.dk, arow < left);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j >> 1 > wk) continue;
+                GdnFrag<NT> fb;
+                if constexpr (NT == 1) {
+                    fb = gdn_load_frag<1>(sK, j * KTN + kb);
+                } else {
+                    const int row = gdn_row(j, r16);
+                    fb = gdn_row_frag<NT>(static_cast<const VT*>(a.k) + (tq + row) * a.dk, kb, a.dk, row < left);
+                }
+                pn[j] = gdn_mm(fa, fb, pn[j]);
+            }
+        }
         // rows of M against q and k (this wave's own tokens are among the depths that each lane
         // holds of a turned fragment); then dq (in M2) and dk (in M1) without the pairs' part
         const int i0 = gdn_row(w, 4 * g);
@@ -566,8 +578,9 @@ __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
                     const int i = i0 + r;
                     const bool on = cj < i + (half == 0);
                     const float d = gdn_decay(vlh[i], vll[i], vlh[cj], vll[cj]);   // may overflow above the diagonal
-                    to[i * LD + cj] = on ? Z[j][r] * (vb[cj] * d) : 0.f;
-                    to2[i * LD + cj] = on ? Z[j][r] * pn[j][r] : 0.f;
+                    const float z = on ? Z[j][r] * d : 0.f;
+                    to[i * LD + cj] = z * vb[cj];
+                    to2[i * LD + cj] = z * pn[j][r];
                 }
             }
         }
