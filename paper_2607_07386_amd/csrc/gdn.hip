@@ -45,18 +45,35 @@ __global__ __launch_bounds__(256) void gdn_step_kernel(GdnArgs a) {
     const size_t tq = (size_t)(b * a.Hk + hk) * a.T, tv = (size_t)bh * a.T;
     const VT* kp = static_cast<const VT*>(a.k) + tq * a.dk;
     const VT* qp = static_cast<const VT*>(a.q) + tq * a.dk;
-    const VT* vp = static_cast<const VT*>(a.v) + tv * a.dv + col;
+    const VT* vp = static_cast<const VT*>(a.v) + tv * a.dv + (cv ? col : 0);
+    // the next token's values are fetched while this one is reduced (rows past d_k and columns past
+    // d_v read the first ones and are taken as zeros)
+    VT nk[NR], nq[NR];
+    v4f nv;
+    float na, nb;
+    const auto fetch = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < NR; ++i) {
+            const int r = rg + 32 * i < a.dk ? rg + 32 * i : 0;
+            nk[i] = kp[(size_t)t * a.dk + r];
+            nq[i] = qp[(size_t)t * a.dk + r];
+        }
+        nv = ld4v(vp + (size_t)t * a.dv);
+        na = a.alpha[tv + t];
+        nb = a.beta[tv + t];
+    };
+    if (len > 0) fetch(0);
     for (int t = 0; t < len; ++t) {
         float kr[NR], qr[NR];
 #pragma unroll
         for (int i = 0; i < NR; ++i) {
-            const int r = rg + 32 * i;
-            const bool ok = r < a.dk;
-            kr[i] = ok ? to_f32(kp[(size_t)t * a.dk + r]) : 0.f;
-            qr[i] = ok ? to_f32(qp[(size_t)t * a.dk + r]) : 0.f;
+            const bool ok = rg + 32 * i < a.dk;
+            kr[i] = ok ? to_f32(nk[i]) : 0.f;
+            qr[i] = ok ? to_f32(nq[i]) : 0.f;
         }
-        const v4f vt = cv ? ld4v(vp + (size_t)t * a.dv) : v4zero();
-        const float al = a.alpha[tv + t], be = a.beta[tv + t];
+        const v4f vt = v4sel(cv, nv, v4zero());
+        const float al = na, be = nb;
+        fetch(min(t + 1, len - 1));
         v4f u = v4zero(), w = v4zero();
         float kq = 0.f;
 #pragma unroll

@@ -30,9 +30,12 @@ bool valid_sizes(int B, int Hk, int H, int T, int d_k, int d_v) {
            d_k % 4 == 0 && d_k <= 256 && d_v >= 4 && d_v % 4 == 0 && d_v <= 4096 && T <= 1 << 30;
 }
 
-// Tokens up to which the recurrent form is the faster one, without states to
-// keep for a backward: it needs one launch and no workspace.
-bool use_step(int T, bool training) { return !training && T <= 16; }
+// Tokens up to which the recurrent form is the faster one, without states to keep for a
+// backward: one launch, no workspace, and a pass over the tokens one by one, where the
+// chunk form pays for 64 of them.  16 streams of 128 x 128: 17 us at 14 tokens, 18 by
+// chunks; 2048 streams: 175, 168; 256 x 256: 22 us at 16 tokens, 31 at 24, 23 by chunks
+// (16 streams); 735 us at 24, 950 by chunks (2048 streams).
+bool use_step(int T, int d_k, bool training) { return !training && T <= (d_k > 128 ? 20 : 14); }
 
 int check_common(const void* q, const void* k, const void* v, int in_dtype, const float* alpha, const float* beta,
                  const int32_t* lens, int B, int Hk, int H, int T, int d_k, int d_v) {
@@ -113,7 +116,7 @@ size_t sdm_gdn_saved_bytes(int B, int H, int T, int d_k, int d_v) {
 }
 
 size_t sdm_gdn_fwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v, int in_dtype, int training) {
-    if (!valid_sizes(B, Hk, H, T, d_k, d_v) || use_step(T, training != 0)) return 0;
+    if (!valid_sizes(B, Hk, H, T, d_k, d_v) || use_step(T, d_k, training != 0)) return 0;
     return gdn_ws(B, Hk, H, T, d_k, d_v, in_dtype, false).total;
 }
 
@@ -146,7 +149,7 @@ int sdm_gdn_fwd(const void* q, const void* k, const void* v, int in_dtype, const
     a.stateT = stateT;
     a.y = y;
     hipError_t e;
-    if (use_step(T, training)) {
+    if (use_step(T, d_k, training)) {
         SdmProfScope ps(SDM_K_GDN_STEP, st);
         e = sdm_launch_gdn_step(a, st);
         return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_gdn_fwd launch");

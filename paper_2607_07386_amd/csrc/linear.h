@@ -54,8 +54,12 @@ struct LinPlan {
 LinPlan sdm_linear_plan(int I, int J, int steps);
 // bf16 factors (or planes of parts) of any sizes
 hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st);
-// a with up to LIN_SKINNY rows, b [J, R], factors of any types; one launch
+// a or b with up to LIN_SKINNY rows, b [J, R], factors of any types; one launch
+// The outputs go up to it for an fp32 x, which is read once instead of being laid out as parts
+// first (16,384 x 2048 by 64: 82 us, 141 by tiles), and to half of it for a bf16 one (32 outputs:
+// 27 us, 26 by tiles; 64: 42, 29).
 #define LIN_SKINNY 64
+inline bool lin_skinny(int I, int J, bool x_f32) { return I <= LIN_SKINNY || J <= (x_f32 ? LIN_SKINNY : LIN_SKINNY / 2); }
 hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st);
 // an fp32 matrix as np bf16 planes [rows][ld] (np 1: rounded, 3: the parts), zeros past its end
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st);

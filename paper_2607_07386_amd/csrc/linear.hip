@@ -418,10 +418,11 @@ bool even_depth(const LinMat& m, bool tr, int R) {
     return tr ? m.rows >= up && (flat || m.T % BK == 0) : m.cols >= up && (m.d == m.cols || m.d % BK == 0);
 }
 
-// ---------------------------------------------------------------- few rows
-// Up to 64 rows of x (the decode step): bound by reading w once.  A workgroup holds 16
-// outputs; its 8 waves take the depth in turns of 64 (a row's 128-byte line in bf16)
-// and their sums meet in LDS, so a call is one launch.
+// ---------------------------------------------------------------- few rows, few outputs
+// Up to 64 rows of x (the decode step) or up to 64 outputs (the gates' pre-activations, one a
+// head): bound by reading the other factor once.  A workgroup holds 16 rows of that
+// one; its 8 waves take the depth in turns of 64 (a row's 128-byte line in bf16) and their
+// sums meet in LDS, so a call is one launch, and fp32 values become bf16 parts on the way.
 // eight depths of a row, from offsets o0 and o1 (the second four, which may be another
 // head's); zeros where the depth has ended
 template <int NT>
@@ -447,16 +448,20 @@ __device__ __forceinline__ GdnFrag<NT> skinny_frag(const bf16_t* row, int64_t o0
     return f;
 }
 
-template <typename WT, typename XT, int MT, bool FLAT>
+// BT, ST: types of the factor with many rows and of the one with up to 16 MT; X_FLAT: x is [B, T, K];
+// X_MANY: the factor with many rows is x.
+template <typename BT, typename ST, int MT, bool X_FLAT, bool X_MANY>
 __global__ __launch_bounds__(512) void linear_skinny_kernel(LinGemm g) {
-    constexpr int NT = sizeof(WT) == 4 ? 3 : 1;
+    constexpr int NT = sizeof(BT) == 4 && sizeof(ST) == 4 ? 3 : 1;
     __shared__ float red[8][MT][256];
+    const LinMat &big = X_MANY ? g.a : g.b, &few = X_MANY ? g.b : g.a;
+    const int nb = X_MANY ? g.I : g.J, nf = X_MANY ? g.J : g.I;
     const int j0 = blockIdx.x * 16, lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
     // rows past the end repeat the last one: what they give is not stored
-    const WT* wp = static_cast<const WT*>(g.b.p) + (size_t)min(j0 + r16, g.J - 1) * g.R;
-    const XT* xp[MT];
+    const BT* bp = static_cast<const BT*>(big.p) + mat_row(big, min(j0 + r16, nb - 1));
+    const ST* fp[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) xp[m] = static_cast<const XT*>(g.a.p) + mat_row(g.a, min(16 * m + r16, g.I - 1));
+    for (int m = 0; m < MT; ++m) fp[m] = static_cast<const ST*>(few.p) + mat_row(few, min(16 * m + r16, nf - 1));
     sdm_f32x4 acc[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -466,10 +471,11 @@ __global__ __launch_bounds__(512) void linear_skinny_kernel(LinGemm g) {
             const int k = k0 + 32 * h + 8 * q;
             const bool ok0 = k < g.R, ok1 = k + 4 < g.R;
             const int ka = ok0 ? k : 0, kb = ok1 ? k + 4 : 0;
-            const GdnFrag<NT> fw = skinny_frag<NT>(wp, ka, kb, ok0, ok1);
-            const int64_t xa = FLAT ? ka : mat_col(g.a, ka), xb = FLAT ? kb : mat_col(g.a, kb);
+            const int64_t xa = X_FLAT ? ka : mat_col(g.a, ka), xb = X_FLAT ? kb : mat_col(g.a, kb);
+            const GdnFrag<NT> fb = skinny_frag<NT>(bp, X_MANY ? xa : ka, X_MANY ? xb : kb, ok0, ok1);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) acc[m] = gdn_mm(skinny_frag<NT>(xp[m], xa, xb, ok0, ok1), fw, acc[m]);
+            for (int m = 0; m < MT; ++m)
+                acc[m] = gdn_mm(skinny_frag<NT>(fp[m], X_MANY ? ka : xa, X_MANY ? kb : xb, ok0, ok1), fb, acc[m]);
         }
     }
 #pragma unroll
@@ -478,20 +484,29 @@ __global__ __launch_bounds__(512) void linear_skinny_kernel(LinGemm g) {
         for (int r = 0; r < 4; ++r) red[w][m][(4 * q + r) * 16 + r16] = acc[m][r];
     __syncthreads();
     for (int u = threadIdx.x; u < MT * 256; u += 512) {
+        // neighbouring threads store neighbouring outputs
+        const int f = X_MANY ? u % (16 * MT) : u >> 4, b = X_MANY ? u / (16 * MT) : u & 15;
         float c = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c += red[i][u >> 8][u & 255];
-        const int oi = u >> 4, oj = j0 + (u & 15);
+        for (int i = 0; i < 8; ++i) c += red[i][f >> 4][(f & 15) * 16 + b];
+        const int oi = X_MANY ? j0 + b : f, oj = X_MANY ? f : j0 + b;
         if (oi < g.I && oj < g.J) lin_store(g, mat_off(g.out, oi, oj), oj, c);
     }
 }
 
-template <typename WT, typename XT, bool FLAT>
+template <typename WT, typename XT, bool X_FLAT>
 hipError_t launch_skinny_rows(const LinGemm& g, hipStream_t st) {
-    const int grid = (g.J + 15) / 16;
-    if (g.I <= 16) linear_skinny_kernel<WT, XT, 1, FLAT><<<grid, 512, 0, st>>>(g);
-    else if (g.I <= 32) linear_skinny_kernel<WT, XT, 2, FLAT><<<grid, 512, 0, st>>>(g);
-    else linear_skinny_kernel<WT, XT, 4, FLAT><<<grid, 512, 0, st>>>(g);
+    if (g.I <= LIN_SKINNY) {
+        const int grid = (g.J + 15) / 16;
+        if (g.I <= 16) linear_skinny_kernel<WT, XT, 1, X_FLAT, false><<<grid, 512, 0, st>>>(g);
+        else if (g.I <= 32) linear_skinny_kernel<WT, XT, 2, X_FLAT, false><<<grid, 512, 0, st>>>(g);
+        else linear_skinny_kernel<WT, XT, 4, X_FLAT, false><<<grid, 512, 0, st>>>(g);
+    } else {
+        const int grid = (g.I + 15) / 16;
+        if (g.J <= 16) linear_skinny_kernel<XT, WT, 1, X_FLAT, true><<<grid, 512, 0, st>>>(g);
+        else if (g.J <= 32) linear_skinny_kernel<XT, WT, 2, X_FLAT, true><<<grid, 512, 0, st>>>(g);
+        else linear_skinny_kernel<XT, WT, 4, X_FLAT, true><<<grid, 512, 0, st>>>(g);
+    }
     return hipGetLastError();
 }
 template <typename WT, typename XT>

@@ -71,7 +71,7 @@ size_t split_bytes(const LinPlan& p, int I, int J) { return p.split > 1 ? (size_
 
 Ws fwd_ws(int x_dtype, int w_dtype, int M, int K, int N) {
     Ws s;
-    if (M <= LIN_SKINNY) return s;
+    if (lin_skinny(M, N, x_dtype == SDM_F32)) return s;
     if (x_dtype == SDM_F32) s.x = s.take(planes(parts_of(w_dtype), M, K));
     if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
     s.py = sdm_linear_plan(M, N, steps_of(K, w_dtype));
@@ -145,7 +145,7 @@ int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dty
     g.split = 1;
     SdmProfScope ps(SDM_K_LINEAR, st);
     hipError_t e = hipSuccess;
-    if (M <= LIN_SKINNY) {
+    if (lin_skinny(M, N, x_dtype == SDM_F32)) {
         e = sdm_launch_linear_skinny(g, st);
         return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear launch");
     }

@@ -613,9 +613,12 @@ def scan_bwd(w_idx, w_val, r_idx, r_val, v, alpha, beta, mem, saved, dy, dmem_T=
     return out
 
 
+_HERE_ALREADY = contextlib.nullcontext()
+
+
 def _current(dev):
     """Context in which `dev` is the current device (launches go to the current one)."""
-    return torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else contextlib.nullcontext()
+    return torch.cuda.device(dev) if dev.index != torch.cuda.current_device() else _HERE_ALREADY
 
 
 def _check_gdn(q, k, v, alpha, beta, lens):
@@ -666,12 +669,13 @@ def gdn_fwd(q, k, v, alpha, beta, state0=None, lens=None, saved=None, workspace=
     code = _dtype_code(q)
     need = lib().sdm_gdn_fwd_workspace_bytes(B, Hk, H, T, dk, dv, code, int(saved is not None))
     _check_ws(workspace, need)
-    _check_ws(saved, lib().sdm_gdn_saved_bytes(B, H, T, dk, dv), "saved")
+    if saved is not None:
+        _check_ws(saved, lib().sdm_gdn_saved_bytes(B, H, T, dk, dv), "saved")
     dev = _dev(q, k, v, alpha, beta, lens, state0, state_out, saved, workspace, y)
     if y is None:
-        y = (torch.empty if lens is None else torch.zeros)((B, H, T, dv), dtype=torch.float32, device=dev)
+        y = alpha.new_empty((B, H, T, dv)) if lens is None else alpha.new_zeros((B, H, T, dv))
     if state_out is None:
-        state_out = torch.empty((B, H, dk, dv), dtype=torch.float32, device=dev)
+        state_out = alpha.new_empty((B, H, dk, dv))
     if workspace is None and need:
         workspace = _ws(need, dev)
     with _current(dev):

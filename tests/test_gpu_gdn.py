@@ -60,7 +60,8 @@ def close(got, ref, what, tol=TOL):
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("B,Hk,H,T,dk,dv", [
-    (1, 1, 1, 1, 4, 4), (3, 2, 4, 1, 128, 128), (2, 1, 3, 2, 36, 100), (1, 2, 2, 16, 256, 64), (2, 2, 2, 17, 128, 128),
+    (1, 1, 1, 1, 4, 4), (3, 2, 4, 1, 128, 128), (2, 1, 3, 2, 36, 100), (1, 2, 2, 16, 256, 64), (2, 2, 2, 17, 128, 128), (2, 1, 2, 14, 64, 36), (2, 1, 2, 15, 64, 36),
+    (1, 1, 2, 20, 256, 36), (1, 1, 2, 21, 256, 36),
     (1, 1, 2, 63, 32, 32), (1, 2, 2, 64, 64, 20), (2, 1, 1, 65, 68, 132), (1, 1, 1, 129, 4, 4), (1, 1, 2, 200, 132, 64),
     (1, 1, 1, 150, 256, 260), (2, 2, 6, 333, 96, 48),
 ])

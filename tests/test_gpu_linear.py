@@ -54,7 +54,8 @@ def reference(x, w, bias, act, residual, hout):
 SHAPES = [  # B, T, K, N, heads in, heads out
     (1, 1, 8, 1, 0, 0), (3, 1, 64, 7, 0, 7), (16, 1, 256, 512, 0, 4), (2, 33, 40, 130, 5, 0), (1, 129, 136, 65, 0, 5),
     (2, 257, 96, 96, 2, 3), (1, 300, 704, 260, 0, 0), (3, 50, 520, 24, 13, 12), (1, 640, 512, 512, 8, 8),
-    (5, 1, 1024, 1, 0, 0), (2, 512, 256, 384, 2, 6), (1, 1, 4096, 300, 0, 0),
+    (5, 1, 1024, 1, 0, 0), (2, 512, 256, 384, 2, 6), (1, 1, 4096, 300, 0, 0), (1, 64, 72, 40, 3, 2), (1, 65, 72, 32, 0, 4),
+    (3, 50, 72, 33, 9, 0), (2, 65, 200, 64, 5, 4), (1, 33, 1000, 50, 0, 0),
 ]
 
 
