@@ -39,7 +39,8 @@
  *     of the workspace and synchronises the stream; without it a repeated id
  *     is undefined behaviour and an id out of range is clamped and flagged.
  *   - dtype codes: SDM_F32 (IEEE fp32) or SDM_BF16 (bfloat16).  Memory
- *     tables, outputs and gradients are always fp32.
+ *     tables, states, outputs and gradients are always fp32, but for the
+ *     projections' (sdm_linear), which state theirs.
  */
 #ifndef SDM_H_
 #define SDM_H_
@@ -305,8 +306,8 @@ size_t sdm_scan_bwd_workspace_bytes(int B, int H, int T, int W, int R, int d_v);
  * sdm_gates — the gate producers of Sec. 3.1 step 2, per head and token:
  *   alpha = exp(-A[h] softplus(a + b_dt[h]))   (forget gate)
  *   beta  = sigma(b)                           (input gate)
- * from the pre-activations a = W_a x and b = W_b x, which the caller's input
- * projection GEMM produces.  A is the learnable decay (Sec. 4 initialises it
+ * from the pre-activations a = W_a x and b = W_b x, one output a head of the
+ * input projection (sdm_linear).  A is the learnable decay (Sec. 4 initialises it
  * in [0, 16]), b_dt the time-step bias (inverse softplus of [0.001, 0.1]).
  *   a_pre, b_pre  [B, H, T] in dtype;  A, b_dt [H] fp32;
  *   alpha, beta   out [B, H, T] fp32.
@@ -327,8 +328,8 @@ int sdm_gates_bwd(const void* a_pre, const void* b_pre, int dtype, const float* 
  * Head Mixing") and Fig. 2's g (.) Norm(y): per (b, h, t) row of d_v values
  *   rstd = 1 / sqrt(mean_c y[c]^2 + eps),  o[c] = y[c] rstd gamma[c] phi(g[c]),
  * phi = identity (act = 0, the element-wise gate as the text states it) or
- * SiLU g sigma(g) (act = 1).  W_o, which mixes the heads afterwards, is a
- * plain GEMM outside this library.
+ * SiLU g sigma(g) (act = 1).  W_o, which mixes the heads afterwards, is
+ * sdm_linear on o as it stands.
  *   y      [B, H, T, d_v] fp32 (the read of Eq. sdm-read);
  *   g      [B, H, T, d_v] in g_dtype: the output gate W_g x;
  *   gamma  [d_v] fp32 norm scale shared by the heads, or NULL (ones);
