@@ -59,7 +59,8 @@ struct GdnArgs {
     float* dS;                     // [B H nC][dk][dv] adjoints at the chunks' ends (backward)
     // the forward scan in `segs` segments of `seg_len` chunks each (1: the whole sequence):
     int segs, seg_len;
-    float* seg_z;                  // [segs - 1][B H][dk][dv] a segment's end from the zero state, then from its true start
+    float* seg_z;                  // [segs][B H][dk][dv] a segment's end from the zero state, then from its true
+                                   // start; in the last place the start of the sequence
     float* seg_phi;                // [segs - 1][B H][dk][dk] what it multiplies its start by
 };
 

@@ -560,8 +560,11 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
 #pragma unroll
             for (int r = 0; r < 4; ++r) S[d][r] = unit && gdn_row(h * KTN + d, 4 * g + r) == col ? 1.f : 0.f;
     } else {
-        gdn_load_state(S, seg ? a.seg_z + ((size_t)(seg - 1) * BH + bh) * sn : a.state0 ? a.state0 + bh * sn : nullptr, h * KTN,
-                       a.dk, a.dv, co);
+        // segments side by side: the first one's start is the join's copy, since another segment's
+        // workgroup may have stored stateT, which may be state0, before this one begins
+        const float* s0 = a.segs > 1 ? a.seg_z + ((size_t)(seg ? seg - 1 : a.segs - 1) * BH + bh) * sn
+                                     : a.state0 ? a.state0 + bh * sn : nullptr;
+        gdn_load_state(S, s0, h * KTN, a.dk, a.dv, co);
     }
     const auto give_state = [&]() {
 #pragma unroll
@@ -752,6 +755,7 @@ __global__ __launch_bounds__(256) void gdn_join_kernel(GdnArgs a) {
     const int d0 = KTN == 2 ? 2 * w : w * N;
     const bool holds = KTN > 2 || w < 2;
     gdn_load_state(S, a.state0 && holds ? a.state0 + bh * sn : nullptr, d0, a.dk, a.dv, co);
+    if (holds) gdn_store_state(S, a.seg_z + ((size_t)(a.segs - 1) * BH + bh) * sn, d0, a.dk, a.dv, co);
     for (int s = 0; s + 1 < a.segs; ++s) {
         uint16_t* f = sS[s & 1];
         const size_t at = (size_t)s * BH + bh;
@@ -846,7 +850,7 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
     w.seg_len = (int)((nC + w.segs - 1) / w.segs);
     if (w.seg_len > 0) w.segs = (int)((nC + w.seg_len - 1) / w.seg_len);
     if (w.segs > 1) {
-        w.seg_z = take((size_t)(w.segs - 1) * B * H * dk * dv * 4);
+        w.seg_z = take((size_t)w.segs * B * H * dk * dv * 4);
         w.seg_phi = take((size_t)(w.segs - 1) * B * H * dk * dk * 4);
     }
     w.kt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);

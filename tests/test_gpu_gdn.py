@@ -103,6 +103,19 @@ def test_few_streams_in_segments(dk, dv, bf16):
     assert torch.equal(S, mine)
 
 
+def test_state_in_place_with_segments_that_some_sequences_do_not_reach():
+    """More workgroups than the device holds at once, many with nothing to do but store the last state
+    before the first segment's have begun: in place as into another buffer."""
+    a, s0, _, _ = inputs(24, 1, 1, 5120, 128, 128, True, seed=9)
+    lens = torch.tensor([5120, 100, 0, 1500] * 6, dtype=torch.int32, device=DEV)
+    y, S = sdm.gdn_fwd(**a, state0=s0, lens=lens)
+    for _ in range(3):
+        mine = s0.clone()
+        y2, S2 = sdm.gdn_fwd(**a, state0=mine, state_out=mine, lens=lens)
+        assert S2 is mine and torch.equal(y, y2) and torch.equal(S, mine)
+    assert torch.equal(S[2], s0[2])
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("B,H,dk,dv", [(16, 32, 32, 32), (16, 16, 64, 32), (32, 16, 100, 32), (16, 16, 128, 36),
                                        (16, 16, 256, 32)])
