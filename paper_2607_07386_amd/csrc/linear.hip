@@ -206,7 +206,7 @@ struct LinTile {
     static constexpr int PPR = (TR ? O : BK) / 8;      // pieces of a row of the tile in LDS
     static constexpr int RPR = 64 / PPR;               // rows of a run
     static constexpr int MASK = PPR / 4 - 1;           // TR: 4 pieces (32 outputs) move together
-    const bf16_t* base;      // EVEN, !TR: start of the first row's sequence; else of the matrix
+    const bf16_t* base;      // EVEN, !TR: the first row (one sequence) or the start of its sequence; else the matrix
     uint32_t off[RUNS];      // EVEN: the lane's rows (!TR) or columns (TR)
     const bf16_t* at[RUNS];  // !EVEN, !TR: the lane's rows (NULL past the end)
 
@@ -219,12 +219,12 @@ struct LinTile {
     __device__ __forceinline__ void init(const LinMat& m, int o0) {
         base = static_cast<const bf16_t*>(m.p);
         if constexpr (EVEN && !TR) {
-            const int seq = o0 / m.T;
-            base += (int64_t)seq * m.sb;
+            const int seq = o0 / m.T, first = m.T == m.rows ? o0 : 0;   // 32 bits reach from there, not from the matrix
+            base += (int64_t)seq * m.sb + (int64_t)first * m.st;
 #pragma unroll
             for (int i = 0; i < RUNS; ++i) {
                 const int o = o0 + (run0() + i) * RPR + row();
-                off[i] = o < m.rows ? (uint32_t)((int64_t)(o / m.T - seq) * m.sb + (int64_t)(o % m.T) * m.st) * 2 : LIN_OUT;
+                off[i] = o < m.rows ? (uint32_t)((int64_t)(o / m.T - seq) * m.sb + (int64_t)(o % m.T - first) * m.st) * 2 : LIN_OUT;
             }
         } else if constexpr (EVEN) {
 #pragma unroll
@@ -422,11 +422,13 @@ hipError_t launch_tile(const LinGemm& g, hipStream_t st) {
 }
 
 // Whether every 64 depths of a factor follow one another in memory, up to a multiple of
-// 64, and 32-bit offsets reach a tile from the start of its first row's sequence.
+// 64, and 32-bit offsets reach a tile: its rows from the first one, or from the start of that one's
+// sequence where there are several; its depths and the columns of every head.
 bool even_depth(const LinMat& m, bool tr, int R) {
     const int up = (R + BK - 1) / BK * BK, span = tr ? BK : 256;
-    const bool flat = m.T == m.rows;
-    const int64_t reach = flat ? (int64_t)span * m.st + m.cols : (int64_t)(span / m.T + 2) * m.sb;
+    const bool flat = m.T == m.rows;   // one sequence
+    const int64_t heads = m.d == m.cols ? m.cols : m.cols / m.d * m.sh;
+    const int64_t reach = tr ? span * m.st + heads : (flat ? span * m.st : (span / m.T + 2) * m.sb) + BK;
     if (reach * 2 >= (int64_t)1 << 31) return false;
     return tr ? m.rows >= up && (flat || m.T % BK == 0) : m.cols >= up && (m.d == m.cols || m.d % BK == 0);
 }

@@ -140,6 +140,36 @@ def test_gradients_against_differences():
             assert abs(got.sum() - d) <= F32_TOL * got.abs().sum(), name
 
 
+@pytest.mark.parametrize("heads", [0, 8])
+def test_more_than_2_gib(heads):
+    """1,049,000 rows of 1024 bf16 values: offsets within x, and within dy, that pass 31 bits (rows flat, heads
+    head-major).  Gradients whose dy is zero but for a few rows need only those."""
+    M, K, N = 1049000, 1024, 64
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randint(-8, 9, (M, K), generator=g, device=DEV, dtype=torch.int8).to(torch.bfloat16) / 8
+    w = (torch.randint(-8, 9, (N, K), generator=g, device=DEV) / 64).to(torch.bfloat16)
+    assert x.numel() * 2 > 2 ** 31
+    at = torch.tensor([0, 1, 255, 256, M // 2, M - 300, M - 2, M - 1], device=DEV)
+    rows, wd = x[at].double(), w.double()
+    lay = (lambda t: t.view(1, M, heads, -1).transpose(1, 2).contiguous()) if heads else (lambda t: t[None])
+    xl = lay(x)
+    y = sdm.linear(xl, w, out_dtype=torch.float32)
+    close(y[0, at], rows @ wd.T, "y", F32_TOL)
+    dy = torch.zeros((1, M, N), dtype=torch.bfloat16, device=DEV)
+    dy[0, at] = (torch.randint(-8, 9, (len(at), N), generator=g, device=DEV) / 8).to(torch.bfloat16)
+    del y
+    out = sdm.linear_bwd(xl, w, dy)
+    close(out["dw"], dy[0, at].double().T @ rows, "dw", BF16_TOL)
+    dx = out["dx"].transpose(1, 2)[0, at].flatten(1) if heads else out["dx"][0, at]
+    close(dx, dy[0, at].double() @ wd, "dx", BF16_TOL)
+    del out, dx
+    # the other way round: the 1024 values are the outputs (wide dy)
+    wt = w.T.contiguous()
+    out = sdm.linear_bwd(dy, wt, xl)
+    close(out["dx"][0, at], rows @ wd.T, "dx of wide outputs", BF16_TOL)
+    close(out["dw"], rows.T @ dy[0, at].double(), "dw of wide outputs", BF16_TOL)
+
+
 def test_no_tokens():
     w, b = torch.randn(24, 16, device=DEV), torch.randn(24, device=DEV)
     x = torch.empty((2, 0, 16), device=DEV)
