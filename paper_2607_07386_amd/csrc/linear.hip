@@ -696,11 +696,12 @@ hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, vo
     return hipGetLastError();
 }
 
-// Rows of a dz workgroup (a multiple of 8, at most 128): four workgroups to a compute unit where
-// the matrix is large enough.
+// Rows of a dz workgroup (a multiple of 8): four workgroups to a compute unit where the matrix is
+// large enough, 128 rows at most, or as many as a grid's 65,535 blocks of rows need.
 static int dz_rows(int rows, int ld) {
     const int64_t want = 4 * (sdm_device_simds() / 4), cb = (ld + 255) / 256;
-    return (int)std::max<int64_t>(8, std::min<int64_t>(128, (int64_t)rows * cb / want / 8 * 8));
+    const int64_t least = ((int64_t)rows + 65534) / 65535;
+    return (int)std::max<int64_t>((least + 7) / 8 * 8, std::min<int64_t>(128, (int64_t)rows * cb / want / 8 * 8));
 }
 int sdm_linear_dz_parts(int rows, int ld) { return (rows + dz_rows(rows, ld) - 1) / dz_rows(rows, ld); }
 

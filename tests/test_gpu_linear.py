@@ -170,6 +170,19 @@ def test_more_than_2_gib(heads):
     close(out["dw"], rows.T @ dy[0, at].double(), "dw of wide outputs", BF16_TOL)
 
 
+def test_bias_gradient_of_many_tokens():
+    """9,000,000 tokens: more blocks of 128 rows than a grid takes in one direction.  Terms of one sign, each
+    in at most 144 / 8 + 8 + 65,535 / 32 + 32 additions: off by 2106 roundings of 2^-24 of the sum at most."""
+    M, N = 9000000, 8
+    g = torch.Generator(device=DEV).manual_seed(5)
+    x = torch.ones((1, M, 8), dtype=torch.bfloat16, device=DEV)
+    w = torch.eye(8, dtype=torch.bfloat16, device=DEV)
+    dy = torch.rand((1, M, N), generator=g, device=DEV) + 0.5
+    out = sdm.linear_bwd(x, w, dy, want_dw=False, want_dbias=True)
+    close(out["dbias"], dy[0].double().sum(0), "dbias", 2106 * 2.0 ** -24)
+    close(out["dx"][0, -1000:], dy[0, -1000:].double(), "dx", 2 * 2.0 ** -8)
+
+
 def test_no_tokens():
     w, b = torch.randn(24, 16, device=DEV), torch.randn(24, device=DEV)
     x = torch.empty((2, 0, 16), device=DEV)
