@@ -474,7 +474,8 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  * y may be residual; no other output may overlap an input.
  *   workspace  at least sdm_linear_workspace_bytes() bytes, 256-B aligned;
  *              NULL where that is 0.
- * Limits: K and K / x_heads multiples of 8 (bf16 w) or 4 (fp32); B T <= 2^30.
+ * Limits: K and K / x_heads multiples of 8 (bf16 w) or 4 (fp32); B T <= 2^26;
+ *         K <= 2^24, N <= 2^22.
  *
  * sdm_linear_bwd — reverse mode, with dz = dy act'(z):
  *   dx = dz W,  dw = dz^T x,  dbias[n] = sum over tokens of dz;  the gradient of

@@ -44,7 +44,8 @@ const char* bad_sizes(int x_dtype, int x_heads, int w_dtype, int act, int B, int
     return nullptr;
 }
 const char* too_large(int B, int T, int K, int N) {
-    if ((int64_t)B * T > (1 << 30)) return "B*T must be <= 2^30";
+    // 16 rows a workgroup of 512 threads, and a launch holds fewer than 2^32 threads
+    if ((int64_t)B * T > (1 << 26)) return "B*T must be <= 2^26";
     if (K > (1 << 24) || N > (1 << 22)) return "K must be <= 2^24, N <= 2^22";
     return nullptr;
 }

@@ -25,7 +25,7 @@ def bwd(**kw):
 
 SIZES = [(dict(B=-1), -1), (dict(T=-1), -1), (dict(K=0), -1), (dict(N=0), -1), (dict(K=60), -1), (dict(K=66), -1),
          (dict(xd=2), -1), (dict(wd=-1), -1), (dict(wd=0), -1), (dict(act=3), -1), (dict(act=-1), -1), (dict(xh=3), -1),
-         (dict(xh=16), -1), (dict(yh=7), -1), (dict(xh=-1), -1), (dict(yh=-1), -1), (dict(B=1 << 20, T=1 << 20), -2),
+         (dict(xh=16), -1), (dict(yh=7), -1), (dict(xh=-1), -1), (dict(yh=-1), -1), (dict(B=1 << 20, T=1 << 20), -2), (dict(B=1 << 13, T=(1 << 13) + 1), -2),
          (dict(K=(1 << 24) + 8), -2), (dict(N=(1 << 22) + 1), -2), (dict(x=None), -1), (dict(w=None), -1),
          (dict(x=A + 8), -1), (dict(w=A + 2), -1)]
 
