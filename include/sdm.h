@@ -428,7 +428,10 @@ int sdm_layer_bwd(const void* cb_q, const void* cb_k, int cb_dtype, int d_k,
  * are logarithms: a gate below 1e-20 counts as 1e-20 there.  All products are
  * fp32 (bf16 inputs are exact); the two forms agree to rounding.  Results do not
  * depend on scheduling and are the same from run to run.
- * Limits: d_k, d_v % 4 == 0; d_k <= 256; d_v <= 4096; B H <= 65535.
+ * An infinity or NaN among a sequence's tokens may reach, as NaN, every output of the
+ * heads that read it in the same 64 tokens (those before it too) and all that follow; tokens past
+ * lens are not read.  y, saved and the workspace overlap no input.
+ * Limits: d_k, d_v % 4 == 0; d_k <= 256; d_v <= 4096; B H <= 65535; T <= 2^30.
  * ---------------------------------------------------------------------- */
 int sdm_gdn_fwd(const void* q, const void* k, const void* v, int in_dtype, const float* alpha, const float* beta,
                 const int32_t* lens, const float* state0, float* stateT, int B, int Hk, int H, int T, int d_k,
@@ -471,7 +474,8 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *             out beside a bf16 z: what its rounding left, in bf16.
  * Sums are fp32; bf16 products are exact, fp32 ones fp32.  Sums over split
  * depths are added in a fixed order: results are the same from run to run.
- * y may be residual; no other output may overlap an input.
+ * y may be residual; no other output may overlap an input.  An infinite fp32 factor of
+ * fp32 products counts as NaN; a token's stay in its own outputs.
  *   workspace  at least sdm_linear_workspace_bytes() bytes, 256-B aligned;
  *              NULL where that is 0.
  * Limits: K and K / x_heads multiples of 8 (bf16 w) or 4 (fp32); B T <= 2^26;

@@ -756,6 +756,8 @@ def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dty
     heads = int(heads)
     if heads < 0 or (heads and N % heads):
         raise ValueError(f"heads {heads} must divide the {N} outputs")
+    if want_rest and not want_z:
+        raise ValueError("want_rest goes with want_z")
     if bias is not None:
         _expect(bias, "bias", (N,), _F32)
     dt = w.dtype if out_dtype is None else out_dtype

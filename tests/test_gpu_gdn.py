@@ -274,6 +274,20 @@ def test_a_sequence_in_parts_and_token_by_token():
     close(St, S.double(), "state")
 
 
+@pytest.mark.parametrize("what", ["v", "k", "alpha"])
+def test_nan_stays_in_its_heads_and_chunk_on(what):
+    a, s0, _, _ = inputs(1, 2, 4, 200, 64, 32, True)
+    y0, S0 = sdm.gdn_fwd(**a, state0=s0)
+    a[what][0, 1, 100] = float("nan")      # v, alpha: head 1; k: the key head of heads 2 and 3
+    y, S = sdm.gdn_fwd(**a, state0=s0)
+    hit = [2, 3] if what == "k" else [1]
+    for h in range(4):
+        if h in hit:
+            assert torch.equal(y[0, h, :64], y0[0, h, :64]) and torch.isnan(y[0, h, 101:]).any()
+        else:
+            assert torch.equal(y[0, h], y0[0, h]) and torch.equal(S[0, h], S0[0, h])
+
+
 def test_same_from_run_to_run_and_on_another_stream():
     a, s0, dy, _ = inputs(2, 2, 4, 300, 128, 64, True)
     saved = sdm.gdn_saved_buffer(2, 4, 300, 128, 64, torch.device(DEV))

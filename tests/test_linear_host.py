@@ -61,7 +61,7 @@ def _t(*s, dt=torch.float32):
     dict(x=_t(5, 16)), dict(x=_t(2, 5, 24)), dict(w=_t(12, 16).double()), dict(x=_t(2, 5, 16, dt=torch.bfloat16)),
     dict(bias=_t(11)), dict(bias=_t(12, dt=torch.bfloat16)), dict(residual=_t(2, 5, 16)), dict(heads=5), dict(heads=-1),
     dict(residual=_t(2, 5, 12), heads=3), dict(out_dtype=torch.bfloat16), dict(out_dtype=torch.float16),
-    dict(y=_t(2, 5, 13)), dict(y=_t(2, 3, 5, 4)), dict(workspace=_t(4)), dict(x=[1])])
+    dict(y=_t(2, 5, 13)), dict(y=_t(2, 3, 5, 4)), dict(workspace=_t(4)), dict(x=[1]), dict(want_rest=True)])
 def test_binding_refuses(kw):
     a = dict(x=_t(2, 5, 16), w=_t(12, 16))
     a.update(kw)
