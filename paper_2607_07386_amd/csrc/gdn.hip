@@ -27,8 +27,8 @@ namespace {
 
 // ---------------------------------------------------------------- recurrent
 // A workgroup holds 32 columns of one stream: 8 quads of columns x 32 row
-// groups, rows rg + 32 i in registers.  One token of 256 streams of 128 x 128: 8.2 us, 4.1 TB/s
-// (the state read and written once, a copy's rate being 4.7); of 16 streams 4.4 us, a launch.
+// groups, rows rg + 32 i in registers.  One token of 256 streams of 128 x 128: 7.9 us, 4.3 TB/s
+// (the state read and written once, a copy's rate being 4.8); of 16 streams 4.0 us, a launch.
 template <typename VT, int NR>
 __global__ __launch_bounds__(256) void gdn_step_kernel(GdnArgs a) {
     __shared__ float red[2][4][8][9];
@@ -158,7 +158,7 @@ __device__ __forceinline__ sdm_f32x4 lds_mm16(const float* A, int ar, int ac, co
 // products, T'_21 = -T'_22 A_21 T'_11, first within each half, then between.
 // Everything is latency, so what counts is how many workgroups share a compute unit:
 // one 64x64 matrix in LDS serves A, then T' in its place, then P (23 KB, five workgroups).
-// 8192 chunks of d_k = 128: 117 us, 0.44 GB moved, 3.8 TB/s (329 us with three matrices
+// 8192 chunks of d_k = 128: 122 us, 0.44 GB moved, 3.6 TB/s (329 us with three matrices
 // and K^T gathered for the scan, two workgroups).
 template <typename VT, int KTN, bool BWD>
 __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
@@ -495,9 +495,10 @@ __global__ __launch_bounds__(256, 1) void gdn_scan_wide_kernel(GdnArgs a) {
 // other (the state's fragments, R and E of the first 32 tokens, E for the update)
 // passes through LDS.  The chunk's K, Q, T' and P are fetched into registers a chunk
 // ahead and staged once for the workgroup; K^T is K read with the transposing loads.
-// 128 streams of 4096 tokens, 128 x 128: 313 us, 4.9 us a chunk.  Two waves share a SIMD
-// there, each with 108 matrix instructions (1.44 us for both) and 416 vector ones (1.4 us), and LDS
-// is busy for 1.7 us: three pipes near each other's pace and four barriers between
+// 128 streams of 4096 tokens, 128 x 128: 305 us in a short run, 4.8 us a chunk (350 in
+// a long one).  Two waves share a SIMD there; a chunk takes each 108 matrix instructions, which
+// keep the matrix pipe for 1,720 cycles, and 420 vector ones, and its unit's LDS 4,130 cycles (bank
+// conflicts 770): pipes near each other's pace and four barriers between
 // dependent stages.  HBM sees 0.62 GB (2.0 TB/s).  16 streams, 128 column tiles in all: 3.5 us a chunk,
 // the chain of dependent products.  (A wave to 16 columns took 6.2 us a chunk.)
 template <typename VT, int KTN, int NCT_>
@@ -740,7 +741,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
 // Starts of the segments, one after the other: S_{s+1} = Phi_s S_s + Z_s in Z_s's place.  A workgroup takes
 // 16 columns of a stream, its four waves a quarter of the rows each; the state passes from
 // segment to segment as fragments in LDS (two of them, one barrier a segment).  Seven joins of 16
-// streams: 42 us, each a read of Phi that waits for nothing but is not fetched ahead.
+// streams: 37 us, each a read of Phi that waits for nothing but is not fetched ahead.
 template <int KTN>
 __global__ __launch_bounds__(256) void gdn_join_kernel(GdnArgs a) {
     constexpr int N = KTN / 2;               // row tiles of a wave

@@ -148,8 +148,8 @@ __global__ __launch_bounds__(256, 1) void gdn_adjoint_wide_kernel(GdnArgs a) {
 // Two waves to 16 columns as in the forward scan: half h
 // holds tokens 32 h .. + 31 and one half of the state's rows.  dY is read whole by both
 // (its part below needs no exchange); F = diag(beta) dE of the last 32 tokens and -G dR
-// pass through LDS.  64 streams of 4096 tokens, 128 x 128: 310 us, 4.8 us a chunk, as the forward that
-// keeps its states (330 us); of its bytes (0.6 GB) the states at the chunks' ends are 0.27 GB.
+// pass through LDS.  64 streams of 4096 tokens, 128 x 128: 295 to 310 us, 4.7 us a chunk, as the forward that
+// keeps its states (316 to 330 us); of its bytes (0.6 GB) the states at the chunks' ends are 0.27 GB.
 template <typename VT, int KTN, int NCT_>
 struct AdjCfg {
     static constexpr int NT = GdnIn<VT>::NT;
@@ -388,9 +388,9 @@ constexpr size_t grads_stage(int ktn, bool bf) {
 // d_v the workgroup stages S0, dS1 and X once as fragments in LDS, the next columns'
 // values being fetched meanwhile; a row of a matrix is the same fragment as an A or
 // a B operand, so every product over d_v reads its rows straight from memory.
-// 4096 chunks of 128 x 128: 545 us for 0.80 GB, 1.5 TB/s.  One workgroup holds a compute unit (105 KB
-// of LDS, 183 registers), so its two phases do not overlap another's: the products over d_v
-// take 370 us of it (290 without the matrix instructions, the loads' pace), the pairs 230.
+// 4096 chunks of 128 x 128: 522 to 550 us for 0.80 GB, 1.5 TB/s.  One workgroup holds a compute unit (105 KB
+// of LDS, 183 registers), so its two phases do not overlap another's: timed each by itself, the products
+// over d_v take 370 us (290 without the matrix instructions, the loads' pace), the pairs 230.
 template <typename VT, int KTN>
 __global__ __launch_bounds__(512, 2) void gdn_grads_kernel(GdnArgs a) {
     constexpr int NT = GdnIn<VT>::NT, DT = 2 * KTN, DH = KTN;   // DH: a wave's tiles of 16 columns of d_k

@@ -10,9 +10,9 @@
 // first being turned on its way from LDS.  fp32 factors are cut into three bf16 parts
 // each (gdn.h) and multiplied as six products one after the other in the same
 // accumulators, which is faster than the fp32 matrix instruction.  Measured: 8192^3 in
-// bf16 0.87 ms, 1.26 PFLOP/s, 4096^3 1.21 (the library's product 1.21 to 1.6 there); fp32
-// 4096^3 197 TFLOP/s (the library's 150); a layer's projection, 16,384 tokens of 2048 to
-// 2048 with SiLU, head-major, 155 us, 0.89 PFLOP/s (the library's product alone 103 us).
+// bf16 0.85 ms, 1.29 PFLOP/s (the library's product 1.66); fp32 4096^3 200 TFLOP/s (the
+// library's 151); a layer's projection, 16,384 tokens of 2048 to 2048, 126 us (the library 95),
+// with SiLU, head-major, 152 us, 0.90 PFLOP/s.
 // There the 32 steps of a tile are few beside its start and its epilogue, and 512
 // tiles make two rounds of 256 compute units in which neither overlaps the next.
 #include <algorithm>
@@ -438,7 +438,7 @@ bool even_depth(const LinMat& m, bool tr, int R) {
 // head): bound by reading the other factor once.  A workgroup holds 16 rows of that
 // one; its 8 waves take the depth in turns of 64 (a row's 128-byte line in bf16) and their
 // sums meet in LDS, so a call is one launch, and fp32 values become bf16 parts on the way.
-// 16 rows, 2048 x 2048: 7.0 us (8.4 MB of w, 1.2 TB/s; a launch alone takes 4); 16,384 rows, 16
+// 16 rows, 2048 x 2048: 6.7 us (8.4 MB of w, 1.3 TB/s; a launch alone takes 4); 16,384 rows, 16
 // outputs: 21 us (3.2 TB/s), fp32 35 us (3.9 TB/s).
 // eight depths of a row, from offsets o0 and o1 (the second four, which may be another
 // head's); zeros where the depth has ended
@@ -545,7 +545,7 @@ __device__ __forceinline__ void put_parts(bf16_t* p, int64_t plane, const float 
 }
 
 // An fp32 matrix as bf16 planes [rows][ld], zeros past its end (both multiples of 64).  16,384 x 2048
-// head-major, rounded: 32 us, 6.3 TB/s.
+// head-major, rounded: 32 us, 201 MB (part of it from the caches).
 template <int NP>
 __global__ __launch_bounds__(256) void linear_parts_kernel(LinMat m, int rows, int ld, bf16_t* out, int64_t plane) {
     const int c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(LinMat m, int rows, i
 
 // dz = dy act'(z) as planes [rows][ld] (zeros past M and N) and its column sums over this
 // `per` rows: eight columns a thread, 8 rows at a time.  16,384 x 2048 in bf16 with z and what its
-// rounding left: 71 us, 3.8 TB/s.
+// rounding left: 69 us, 3.9 TB/s.
 template <int NP>
 __global__ __launch_bounds__(256) void linear_dz_kernel(LinMat dy, const void* z, const void* rest, int z_dtype, int act,
                                                         int rows, int per, int ld, bf16_t* dz, int64_t plane,
