@@ -68,4 +68,8 @@ hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, vo
 int sdm_linear_dz_parts(int rows, int ld);
 hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, const void* rest, int z_dtype, int act, int np, int rows, int ld,
                                 void* dz, float* part, float* dbias, hipStream_t st);
+// dw = dz^T x of an fp32 x with g.I <= LIN_SKINNY outputs, from dz's three planes [..][ld], ld a multiple of 64;
+// g: I, J, out, part of g.split = sdm_linear_dw_few_split(M, K)
+int sdm_linear_dw_few_split(int M, int K);
+hipError_t sdm_launch_linear_dw_few(const LinMat& x, const void* dz, int64_t plane, int ld, const LinGemm& g, hipStream_t st);
 hipError_t sdm_launch_linear_zero(void* p, size_t words, hipStream_t st);

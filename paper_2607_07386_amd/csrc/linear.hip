@@ -531,6 +531,63 @@ hipError_t launch_skinny(const LinGemm& g, hipStream_t st) {
     return g.a.d == g.a.cols ? launch_skinny_rows<WT, XT, true>(g, st) : launch_skinny_rows<WT, XT, false>(g, st);
 }
 
+// The weights' gradient of an fp32 projection with few outputs: dw[n, k] = sum over tokens of dz[m, n] x[m, k]
+// is bound by reading x, so x is read once and cut into parts in registers instead of being laid out
+// as parts first.  A workgroup takes 64 columns of x, 16 a wave, and `per` tokens by 128; dz's
+// fragments (its parts are there for dx) are gathered once for its four waves.  The call with dz, its join
+// included: 16,384 x 2048 by 16 63 us (134 MB of x; 148 by tiles), by 64 94 (153 by tiles); 4096 x
+// 1024 by 8 23 (53).
+constexpr int DWF = 128;
+template <int MT>
+__global__ __launch_bounds__(256) void linear_dw_few_kernel(LinMat x, const bf16_t* dz, int64_t plane, int ld, int per, int N,
+                                                            float* part) {
+    __shared__ __align__(16) uint16_t sA[DWF / 32 * MT * 3 * GDN_FRAG];   // [depth block][tile][part]
+    const int lane = lane_id(), w = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+    const int k = blockIdx.x * 64 + 16 * w + r16;
+    const float* xp = static_cast<const float*>(x.p) + mat_col(x, min(k, x.cols - 1));   // columns past the end are not stored
+    const int m1 = min(x.rows, (int)(blockIdx.y + 1) * per);
+    sdm_f32x4 acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = sdm_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int m0 = blockIdx.y * per; m0 < m1; m0 += DWF) {
+        float xv[DWF / 32][8];
+#pragma unroll
+        for (int b = 0; b < DWF / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int m = m0 + 32 * b + 8 * g + i;
+                xv[b][i] = m < m1 ? xp[mat_row(x, m)] : 0.f;
+            }
+        __syncthreads();   // the tokens before
+#pragma unroll
+        for (int f = 0; f < DWF / 32 * MT * 3 / 4; ++f) {
+            const int id = w + 4 * f, p = id % 3, mt = id / 3 % MT, b = id / 3 / MT;
+            lin_us8 v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int m = m0 + 32 * b + 8 * g + i;
+                v[i] = m < m1 ? dz[p * plane + (int64_t)m * ld + 16 * mt + r16].bits : (uint16_t)0;
+            }
+            *reinterpret_cast<lin_us8*>(sA + id * GDN_FRAG + lane * 8) = v;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < DWF / 32; ++b) {
+            const GdnFrag<3> fx = gdn_split(xv[b]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m] = gdn_mm(gdn_load_frag<3>(sA, b * MT + m), fx, acc[m]);
+        }
+    }
+    if (k >= x.cols) return;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int n = 16 * m + 4 * g + r;
+            if (n < N) part[((size_t)blockIdx.y * N + n) * LIN_UP8(x.cols) + k] = acc[m][r];
+        }
+}
+
 // ---------------------------------------------------------------- parts, dz, dbias
 // NP = 1: rounded to bf16; NP = 3: the three bf16 parts of an fp32 value.
 template <int NP>
@@ -687,6 +744,24 @@ hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st) {
     if (g.b.dtype == SDM_DT_F32) return launch_skinny<float, float>(g, st);
     if (g.a.dtype == SDM_DT_F32) return launch_skinny<bf16_t, float>(g, st);
     return launch_skinny<bf16_t, bf16_t>(g, st);
+}
+
+// Parts of the tokens for linear_dw_few_kernel: four workgroups to a compute unit, 256 tokens each or more.
+int sdm_linear_dw_few_split(int M, int K) {
+    const int64_t want = 4 * (sdm_device_simds() / 4) / ((K + 63) / 64), most = ((int64_t)M + 255) / 256;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), 64));
+}
+hipError_t sdm_launch_linear_dw_few(const LinMat& x, const void* dz, int64_t plane, int ld, const LinGemm& g, hipStream_t st) {
+    const int per = ((x.rows + g.split - 1) / g.split + DWF - 1) / DWF * DWF;
+    const dim3 grid((x.cols + 63) / 64, g.split);
+    const bf16_t* d = static_cast<const bf16_t*>(dz);
+    if (g.I <= 16) linear_dw_few_kernel<1><<<grid, 256, 0, st>>>(x, d, plane, ld, per, g.I, g.part);
+    else if (g.I <= 32) linear_dw_few_kernel<2><<<grid, 256, 0, st>>>(x, d, plane, ld, per, g.I, g.part);
+    else linear_dw_few_kernel<4><<<grid, 256, 0, st>>>(x, d, plane, ld, per, g.I, g.part);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    linear_join_kernel<<<dim3((g.J + 255) / 256, (g.I + 7) / 8), 256, 0, st>>>(g);
+    return hipGetLastError();
 }
 
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st) {

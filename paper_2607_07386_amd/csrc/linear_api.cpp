@@ -61,6 +61,7 @@ struct Ws {
     size_t x = 0, w = 0, dz = 0, parts = 0, split = 0, total = 0;
     LinPlan py{}, px{}, pw{};
     bool direct = false;   // dy is dz as it stands
+    bool few = false;      // dw reads x as it stands
     size_t take(size_t bytes) {
         const size_t at = total;
         total += align256(bytes);
@@ -84,12 +85,15 @@ Ws bwd_ws(int x_dtype, int w_dtype, int act, int dy_dtype, int y_heads, int M, i
     const int np = parts_of(w_dtype);
     s.direct = w_dtype == SDM_BF16 && act == 0 && dy_dtype == SDM_BF16 && y_heads == 0 && N % 8 == 0;
     if (!s.direct) s.dz = s.take(planes(np, M, N));
-    if (x_dtype == SDM_F32) s.x = s.take(planes(np, M, K));
+    s.few = w_dtype == SDM_F32 && N <= LIN_SKINNY;
+    if (x_dtype == SDM_F32 && !s.few) s.x = s.take(planes(np, M, K));
     if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
     s.parts = s.take((size_t)sdm_linear_dz_parts(up64(M), up64(N)) * N * 4);
     s.px = sdm_linear_plan(M, K, steps_of(N, w_dtype));
     s.pw = sdm_linear_plan(N, K, steps_of(M, w_dtype));
-    s.split = s.take(std::max(split_bytes(s.px, M, K), split_bytes(s.pw, N, K)));
+    if (s.few) s.pw.split = sdm_linear_dw_few_split(M, K);
+    const size_t dw_bytes = s.few ? (size_t)s.pw.split * N * LIN_UP8(K) * 4 : split_bytes(s.pw, N, K);
+    s.split = s.take(std::max(split_bytes(s.px, M, K), dw_bytes));
     return s;
 }
 // planes of a rows x cols matrix: as rows of a factor (depth = columns), or depth first
@@ -235,7 +239,7 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         g.a = L.direct ? lin_flat(dy, SDM_BF16, M, N, N) : plane_mat(ws + L.dz, M, N, true);
         g.ta = true;
         g.b = lin_tokens(x, x_dtype, B, T, K, x_heads);
-        if (x_dtype == SDM_F32) {
+        if (x_dtype == SDM_F32 && !L.few) {
             e = sdm_launch_linear_parts(g.b, np, up64(M), up64(K), ws + L.x, st);
             g.b = plane_mat(ws + L.x, M, K, true);
             g.plane_b = plane_len(M, K);
@@ -246,7 +250,8 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         g.out = lin_flat(dw, w_dtype, N, K, K);
         g.split = L.pw.split;
         g.big = L.pw.big;
-        if (e == hipSuccess) e = sdm_launch_linear(g, st);
+        if (e == hipSuccess && L.few) e = sdm_launch_linear_dw_few(g.b, ws + L.dz, plane_len(M, N), up64(N), g, st);
+        else if (e == hipSuccess) e = sdm_launch_linear(g, st);
     }
     return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear_bwd launch");
 }

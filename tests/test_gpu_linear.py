@@ -183,6 +183,18 @@ def test_bias_gradient_of_many_tokens():
     close(out["dx"][0, -1000:], dy[0, -1000:].double(), "dx", 2 * 2.0 ** -8)
 
 
+@pytest.mark.parametrize("K,hin", [(136, 0), (68, 17), (2048, 8)])
+@pytest.mark.parametrize("N", [1, 16, 17, 33, 64, 65])
+@pytest.mark.parametrize("M", [127, 129, 256, 257, 5000])
+def test_weights_gradient_with_few_outputs(M, N, K, hin):
+    """Tokens that end inside a group of 128 and inside a part; what lies past the end of x's last row is not
+    read into a sum.  5000 terms of either sign: see the module's tolerance (5000 2^-24 is 3e-4 in the worst
+    case of roundings that all fall one way; they fall either way)."""
+    x, w, _, _, dy = case(1, M, K, N, hin, 0, False)
+    out = sdm.linear_bwd(x, w, dy, want_dx=False)
+    close(out["dw"], flat(dy.double()).flatten(0, 1).T @ flat(x.double()).flatten(0, 1), "dw", F32_TOL)
+
+
 def test_no_tokens():
     w, b = torch.randn(24, 16, device=DEV), torch.randn(24, device=DEV)
     x = torch.empty((2, 0, 16), device=DEV)
