@@ -340,10 +340,10 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
     __syncthreads();
     blocks(a.pf);
     // fp32: K^T and Q^T of the key head, rows of d_k, depth = tokens, for the kernels that do not turn K in LDS
-    if constexpr (NT == 3 && (BWD || KTN == 8)) {
+    if constexpr (NT == 3 && BWD) {
         if (h % G) return;
         const size_t ck = (size_t)(b * a.Hk + hk) * a.nC + c;
-        for (int f = w; f < (BWD ? 2 : 1) * DT * 2; f += 4) {
+        for (int f = w; f < 2 * DT * 2; f += 4) {
             const int id = f % (DT * 2), dt = id >> 1, kb = id & 1;
             const VT* src = f < DT * 2 ? kp : qp;
             const int d = gdn_row(dt, r16);
@@ -359,136 +359,6 @@ __global__ __launch_bounds__(256) void gdn_prep_kernel(GdnArgs a) {
 }
 
 // ---------------------------------------------------------------- scan
-// fp32 inputs with d_k > 128, whose chunk LDS does not hold: one wave per 16 columns, four to a
-// workgroup; the waves
-// share nothing (each reads the chunk's fragments itself) and never wait for
-// one another.  The state stays in the C layout of its own update.
-template <bool SAVE>
-__global__ __launch_bounds__(256, 1) void gdn_scan_wide_kernel(GdnArgs a) {
-    using VT = float;
-    constexpr int NT = 3, KTN = 8, DT = 2 * KTN;
-    const int groups = (a.dv + 63) / 64;
-    int grp, bh;
-    scan_wg_coords<true>(groups, grp, bh);
-    const int col0 = (grp * 4 + (threadIdx.x >> 6)) * 16;
-    if (col0 >= a.dv) return;
-    const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
-    const int lane = lane_id(), r16 = lane & 15, g = lane >> 4;
-    const int col = col0 + r16;
-    const bool cv = col < a.dv;
-    const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
-    const size_t sbase = (size_t)bh * a.dk * a.dv + col;
-    const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-
-    sdm_f32x4 S[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = gdn_row(d, 4 * g + r);
-            S[d][r] = a.state0 && cv && row < a.dk ? a.state0[sbase + (size_t)row * a.dv] : 0.f;
-        }
-    const size_t tq0 = (size_t)(b * a.Hk + hk) * a.T, tv0 = (size_t)bh * a.T;
-    for (int c = 0; c < nc; ++c) {
-        const int t0 = c * GDN_C;
-        const size_t ch = (size_t)bh * a.nC + c, ck = (size_t)(b * a.Hk + hk) * a.nC + c;
-        const VT* kp = static_cast<const VT*>(a.k) + (tq0 + t0) * a.dk;
-        const VT* qp = static_cast<const VT*>(a.q) + (tq0 + t0) * a.dk;
-        const VT* vp = static_cast<const VT*>(a.v) + (tv0 + t0) * a.dv + col;
-        const float* vec = a.vec + ch * GDN_VEC * 64;
-        if constexpr (SAVE) {
-            float* o = a.saved_S + ch * a.dk * a.dv + col;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int row = gdn_row(d, 4 * g + r);
-                    if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
-                }
-        }
-        sdm_f32x4 R[4], Y[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) R[m] = Y[m] = zero;
-#pragma unroll
-        for (int kb = 0; kb < KTN; ++kb) {
-            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int row = gdn_row(m, r16);
-                const bool ok = t0 + row < len;
-                R[m] = gdn_mm(gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, ok), s, R[m]);
-                Y[m] = gdn_mm(gdn_row_frag<NT>(qp + (size_t)row * a.dk, kb, a.dk, ok), s, Y[m]);
-            }
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f gam = ld4(vec + GDN_V_GAM * 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                const float v = cv && t0 + t < len ? to_f32(vp[(size_t)t * a.dv]) : 0.f;
-                R[m][r] = fmaf(-gam[r], R[m][r], v);
-                Y[m][r] *= gam[r];
-            }
-        }
-        sdm_f32x4 X[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) X[m] = zero;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(R[2 * kb], R[2 * kb + 1]);
-#pragma unroll
-            for (int m = 2 * kb; m < 4; ++m)
-                X[m] = gdn_mm(gdn_load_frag<3>(a.tf, ch * GDN_BLKS + gdn_low_blk(m, kb)), f, X[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f be = ld4(vec + GDN_V_BETA * 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                if constexpr (SAVE) {
-                    if (cv && t0 + t < len) a.saved_X[(tv0 + t0 + t) * a.dv + col] = X[m][r];
-                }
-                X[m][r] *= be[r];
-            }
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
-#pragma unroll
-            for (int m = 2 * kb; m < 4; ++m)
-                Y[m] = gdn_mm(gdn_load_frag<3>(a.pf, ch * GDN_BLKS + gdn_low_blk(m, kb)), f, Y[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f en = ld4(vec + GDN_V_END * 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                if (cv && t0 + t < len) a.y[(tv0 + t0 + t) * a.dv + col] = Y[m][r];
-                X[m][r] *= en[r];
-            }
-        }
-        const float last = vec[GDN_V_GAM * 64 + 63];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) S[d] *= last;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(X[2 * kb], X[2 * kb + 1]);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) S[d] = gdn_mm(gdn_load_frag<NT>(a.kt, (ck * DT + d) * 2 + kb), f, S[d]);
-        }
-    }
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = gdn_row(d, 4 * g + r);
-            if (cv && row < a.dk) a.stateT[sbase + (size_t)row * a.dv] = S[d][r];
-        }
-}
-
 // Two waves to 16 columns: half h holds tokens 32 h .. + 31 of the
 // chunk and one half of the state's rows, so that a chunk's chain of dependent products
 // is half as long and twice as many waves share the device.  What a half needs of the
@@ -506,12 +376,15 @@ struct ScanCfg {
     static constexpr int NT = GdnIn<VT>::NT;
     static constexpr int NCT = NCT_;                   // column tiles of a workgroup
     static constexpr int NW = 2 * NCT;
-    static constexpr bool QD = NT == 1 ? KTN == 8 : KTN == 4;   // Q straight from memory: LDS is full
+    static constexpr bool QD = NT == 1 ? KTN == 8 : KTN >= 4;   // Q straight from memory: LDS is full
+    // P as well: K's parts are 96 KB, and it leaves 152 KB in all (256 x 128 in fp32, 16 streams of 384
+    // tokens: 106 us, 301 by a wave to 16 columns that stages nothing; 64 of 1024: 645, 1087)
+    static constexpr bool PD = NT == 3 && KTN == 8;
     static constexpr int FPW = 4 * KTN / NW;           // fragments of K (and Q) that a wave moves
     static constexpr int TPW = (18 + NW - 1) / NW;     // of T' (and P)
     static constexpr int XCH = (KTN + 3) * 3;          // exchanged fragments per column tile: S, then E_a, E'_a, E'_b (R_a)
     static constexpr size_t LDS =
-        (size_t)(4 * KTN * NT * (QD ? 1 : 2) + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+        (size_t)(4 * KTN * NT * (QD ? 1 : 2) + (PD ? 18 : 36) + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
 };
 
 // MODE 0: outputs; 1: and what the backward needs; 2: only a segment's end, from the zero state (columns of
@@ -525,7 +398,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
     uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN][NT]
     uint16_t* sT = sK + 4 * KTN * NT * GDN_FRAG;                 // T' [6][3]
     uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;
-    uint16_t* sX = sP + GDN_BLKS * 3 * GDN_FRAG;            // exchange, per column tile
+    uint16_t* sX = sP + (C::PD ? 0 : GDN_BLKS * 3 * GDN_FRAG);   // exchange, per column tile
     float* sV = reinterpret_cast<float*>(sX + C::NCT * C::XCH * GDN_FRAG);   // [2][gamma, end, beta][64]
     uint16_t* sQ = reinterpret_cast<uint16_t*>(sV + 2 * 3 * 64);             // [4][KTN][NT] unless QD
 
@@ -594,7 +467,16 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
             for (int r = 0; r < 4; ++r) V[m][r] = gdn_ld1<VT>(buf, gdn_row(2 * h + m, 4 * g + r) * a.dv * sizeof(VT) + cov);
     };
     const auto fetch_t = [&](int c) { gdn_fetch_turns<NW>(rT, a.tf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
-    const auto fetch_p = [&](int c) { gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
+    const auto fetch_p = [&](int c) {
+        if constexpr (!C::PD) gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w);
+    };
+    const auto stage_p = [&]() {
+        if constexpr (!C::PD) gdn_stage_turns<NW>(sP, 18, w, rP);
+    };
+    const auto p_frag = [&](int c, int blk) {
+        if constexpr (C::PD) return gdn_load_frag<3>(a.pf, (ch0 + c) * GDN_BLKS + blk);
+        else return gdn_load_frag<3>(sP, blk);
+    };
     const auto stage_k = [&]() { rK.stage(sK, w * C::FPW); };
     const auto stage_q = [&](int par) {
         if constexpr (!C::QD && !STATE) rQ.stage(sQ, w * C::FPW);
@@ -612,7 +494,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
         stage_k();
         stage_q(cb & 1);
         gdn_stage_turns<NW>(sT, 18, w, rT);
-        if constexpr (!STATE) gdn_stage_turns<NW>(sP, 18, w, rP);
+        if constexpr (!STATE) stage_p();
         const int c1 = min(cb + 1, ce - 1);
         fetch_q(c1);
         fetch_t(c1);
@@ -711,10 +593,10 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
             if (h == 1) {
                 const GdnFrag<3> ea = gdn_load_frag<3>(xE, 0);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) Y[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_low_blk(2 + m, 0)), ea, Y[m]);
+                for (int m = 0; m < 2; ++m) Y[m] = gdn_mm(p_frag(c, gdn_low_blk(2 + m, 0)), ea, Y[m]);
             }
 #pragma unroll
-            for (int m = 0; m < 2; ++m) Y[m] = gdn_mm(gdn_load_frag<3>(sP, h ? 3 + 2 * m : m), ef, Y[m]);
+            for (int m = 0; m < 2; ++m) Y[m] = gdn_mm(p_frag(c, h ? 3 + 2 * m : m), ef, Y[m]);
         }
         give_state();
         if constexpr (!STATE) {
@@ -724,7 +606,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_scan_halves_kernel(GdnArgs a
                 for (int r = 0; r < 4; ++r) gdn_stf(ybuf, gdn_row(2 * h + m, 4 * g + r) * a.dv * 4 + co, Y[m][r]);
         }
         __syncthreads();
-        if constexpr (!STATE) gdn_stage_turns<NW>(sP, 18, w, rP);
+        if constexpr (!STATE) stage_p();
         stage_k();
         if constexpr (!STATE) fetch_p(next);
         fetch_k(next);
@@ -797,30 +679,27 @@ hipError_t launch_scan_tiles(const GdnArgs& a, hipStream_t st) {
 // share one staging of the chunk, but also one LDS, whose reads then set the pace.
 template <typename VT, int KTN, int MODE>
 hipError_t launch_scan_halves(const GdnArgs& a, hipStream_t st) {
-    constexpr int MOST = KTN == 2 ? 4 : KTN == 4 && sizeof(VT) == 2 ? 4 : 2;   // what LDS holds
+    constexpr int MOST = KTN == 2 ? 4 : KTN == 4 && sizeof(VT) == 2 ? 4 : KTN == 8 && sizeof(VT) == 4 ? 1 : 2;   // what LDS holds
     const int64_t cols = (a.dv + 15) / 16 + (MODE == 2 ? (a.dk + 15) / 16 : 0);
     const int64_t tiles = cols * a.B * a.H * (MODE == 2 ? a.segs - 1 : a.segs), cus = sdm_device_simds() / 4;
     if constexpr (MOST == 4) {
         if (tiles >= 4 * cus) return launch_scan_tiles<VT, KTN, 4, MODE>(a, st);
     }
-    return tiles >= 2 * cus ? launch_scan_tiles<VT, KTN, 2, MODE>(a, st) : launch_scan_tiles<VT, KTN, 1, MODE>(a, st);
+    if constexpr (MOST >= 2) {
+        if (tiles >= 2 * cus) return launch_scan_tiles<VT, KTN, 2, MODE>(a, st);
+    }
+    return launch_scan_tiles<VT, KTN, 1, MODE>(a, st);
 }
 
 template <typename VT, int KTN, bool SAVE>
 hipError_t launch_scan(const GdnArgs& a, hipStream_t st) {
-    if constexpr (KTN == 8 && sizeof(VT) == 4) {
-        const dim3 grid((a.dv + 63) / 64 * a.B * a.H);
-        gdn_scan_wide_kernel<SAVE><<<grid, 256, 0, st>>>(a);
-        return hipGetLastError();
-    } else {
-        if (a.segs > 1) {
-            hipError_t e = launch_scan_halves<VT, KTN, 2>(a, st);
-            if (e != hipSuccess) return e;
-            gdn_join_kernel<KTN><<<dim3((a.dv + 15) / 16, a.B * a.H), 256, 0, st>>>(a);
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
-        return launch_scan_halves<VT, KTN, SAVE ? 1 : 0>(a, st);
+    if (a.segs > 1) {
+        hipError_t e = launch_scan_halves<VT, KTN, 2>(a, st);
+        if (e != hipSuccess) return e;
+        gdn_join_kernel<KTN><<<dim3((a.dv + 15) / 16, a.B * a.H), 256, 0, st>>>(a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
     }
+    return launch_scan_halves<VT, KTN, SAVE ? 1 : 0>(a, st);
 }
 
 }  // namespace
@@ -847,15 +726,15 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
     w.segs = 1;
     const int64_t tiles = (int64_t)((dv + 15) / 16) * B * H, room = tiles > 0 ? 4 * (sdm_device_simds() / 4) / tiles : 0;
     const int64_t segs = std::min<int64_t>(std::min<int64_t>(room, nC / 16), 64);
-    if (!backward && segs >= 5 && !(f32 && dk > 128)) w.segs = (int)segs;
+    if (!backward && segs >= 5) w.segs = (int)segs;
     w.seg_len = (int)((nC + w.segs - 1) / w.segs);
     if (w.seg_len > 0) w.segs = (int)((nC + w.seg_len - 1) / w.seg_len);
     if (w.segs > 1) {
         w.seg_z = take((size_t)w.segs * B * H * dk * dv * 4);
         w.seg_phi = take((size_t)(w.segs - 1) * B * H * dk * dk * 4);
     }
-    w.kt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
     if (backward) {
+        w.kt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
         w.qt = take(f32 ? nk * dt * 2 * 3 * GDN_FRAG * 2 : 0);
         w.dS = take(n * dk * dv * 4);
     }

@@ -22,7 +22,8 @@
 
 namespace {
 
-// fp32 inputs with d_k > 128: one wave per 16 columns, as gdn_scan_wide_kernel
+// fp32 inputs with d_k > 128, whose chunk LDS does not hold: one wave per 16 columns, four to a workgroup;
+// the waves share nothing (each reads the chunk's fragments itself) and never wait for one another
 __global__ __launch_bounds__(256, 1) void gdn_adjoint_wide_kernel(GdnArgs a) {
     using VT = float;
     constexpr int NT = 3, KTN = 8, DT = 2 * KTN;

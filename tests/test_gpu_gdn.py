@@ -83,7 +83,7 @@ def test_long_memory_many_chunks():
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("dk,dv", [(16, 20), (128, 48)])
+@pytest.mark.parametrize("dk,dv", [(16, 20), (128, 48), (132, 20), (256, 36)])
 def test_few_streams_in_segments(dk, dv, bf16):
     """Long sequences of few streams run segments side by side: a full one, one that ends inside a segment,
     one that ends inside the first, one empty; with the states for a backward too."""
