@@ -22,130 +22,6 @@
 
 namespace {
 
-// fp32 inputs with d_k > 128, whose chunk LDS does not hold: one wave per 16 columns, four to a workgroup;
-// the waves share nothing (each reads the chunk's fragments itself) and never wait for one another
-__global__ __launch_bounds__(256, 1) void gdn_adjoint_wide_kernel(GdnArgs a) {
-    using VT = float;
-    constexpr int NT = 3, KTN = 8, DT = 2 * KTN;
-    const int groups = (a.dv + 63) / 64;
-    int grp, bh;
-    scan_wg_coords<true>(groups, grp, bh);
-    const int col0 = (grp * 4 + (threadIdx.x >> 6)) * 16;
-    if (col0 >= a.dv) return;
-    const int b = bh / a.H, hk = (bh % a.H) / (a.H / a.Hk);
-    const int lane = lane_id(), r16 = lane & 15, g = lane >> 4;
-    const int col = col0 + r16;
-    const bool cv = col < a.dv;
-    const int len = gdn_len(a, b), nc = (len + GDN_C - 1) / GDN_C;
-    const size_t sbase = (size_t)bh * a.dk * a.dv + col;
-    const sdm_f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-
-    sdm_f32x4 S[DT];
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int row = gdn_row(d, 4 * g + r);
-            S[d][r] = a.dstateT && cv && row < a.dk ? a.dstateT[sbase + (size_t)row * a.dv] : 0.f;
-        }
-    const size_t tq0 = (size_t)(b * a.Hk + hk) * a.T, tv0 = (size_t)bh * a.T;
-    for (int c = nc - 1; c >= 0; --c) {
-        const int t0 = c * GDN_C;
-        const size_t ch = (size_t)bh * a.nC + c, ck = (size_t)(b * a.Hk + hk) * a.nC + c;
-        const VT* kp = static_cast<const VT*>(a.k) + (tq0 + t0) * a.dk;
-        const float* vec = a.vec + ch * GDN_VEC * 64;
-        float* o = a.dS + ch * a.dk * a.dv + col;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = gdn_row(d, 4 * g + r);
-                if (cv && row < a.dk) o[(size_t)row * a.dv] = S[d][r];
-            }
-        sdm_f32x4 dE[4], Y[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            dE[m] = zero;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                Y[m][r] = cv && t0 + t < len ? a.dy[(tv0 + t0 + t) * a.dv + col] : 0.f;
-            }
-        }
-#pragma unroll
-        for (int kb = 0; kb < KTN; ++kb) {
-            const GdnFrag<3> s = gdn_stack(S[2 * kb], S[2 * kb + 1]);
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const int row = gdn_row(m, r16);
-                dE[m] = gdn_mm(gdn_row_frag<NT>(kp + (size_t)row * a.dk, kb, a.dk, t0 + row < len), s, dE[m]);
-            }
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f en = ld4(vec + GDN_V_END * 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dE[m][r] *= en[r];
-        }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
-#pragma unroll
-            for (int m = 0; m < 2 * kb + 2; ++m)
-                dE[m] = gdn_mm(gdn_load_frag<3>(a.pf, ch * GDN_BLKS + gdn_up_blk(m, kb)), f, dE[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f be = ld4(vec + GDN_V_BETA * 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dE[m][r] *= be[r];
-        }
-        sdm_f32x4 dR[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) dR[m] = zero;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> f = gdn_stack(dE[2 * kb], dE[2 * kb + 1]);
-#pragma unroll
-            for (int m = 0; m < 2 * kb + 2; ++m)
-                dR[m] = gdn_mm(gdn_load_frag<3>(a.tf, ch * GDN_BLKS + gdn_up_blk(m, kb)), f, dR[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const v4f gam = ld4(vec + GDN_V_GAM * 64 + gdn_row(m, 4 * g));
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int t = gdn_row(m, 4 * g + r);
-                if (cv && t0 + t < len) a.dvv[(tv0 + t0 + t) * a.dv + col] = dR[m][r];
-                dR[m][r] *= -gam[r];
-                Y[m][r] *= gam[r];
-            }
-        }
-        const float last = vec[GDN_V_GAM * 64 + 63];
-#pragma unroll
-        for (int d = 0; d < DT; ++d) S[d] *= last;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const GdnFrag<3> fr = gdn_stack(dR[2 * kb], dR[2 * kb + 1]);
-            const GdnFrag<3> fy = gdn_stack(Y[2 * kb], Y[2 * kb + 1]);
-#pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                S[d] = gdn_mm(gdn_load_frag<NT>(a.kt, (ck * DT + d) * 2 + kb), fr, S[d]);
-                S[d] = gdn_mm(gdn_load_frag<NT>(a.qt, (ck * DT + d) * 2 + kb), fy, S[d]);
-            }
-        }
-    }
-    if (a.dstate0) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int row = gdn_row(d, 4 * g + r);
-                if (cv && row < a.dk) a.dstate0[sbase + (size_t)row * a.dv] = S[d][r];
-            }
-    }
-}
-
 // Two waves to 16 columns as in the forward scan: half h
 // holds tokens 32 h .. + 31 and one half of the state's rows.  dY is read whole by both
 // (its part below needs no exchange); F = diag(beta) dE of the last 32 tokens and -G dR
@@ -159,7 +35,10 @@ struct AdjCfg {
     static constexpr int FPW = 4 * KTN / NW;
     static constexpr int TPW = (18 + NW - 1) / NW;
     static constexpr int XCH = (KTN + 3) * 3;          // S, then F_b, N_a, N_b
-    static constexpr size_t LDS = (size_t)(8 * KTN * NT + 36 + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
+    // K's parts are 96 KB: Q^T (turned already for the gradients) and P^T come straight from memory (256 x 128
+    // in fp32, 16 streams of 384 tokens: the backward 256 us, 432 by a wave to 16 columns that stages nothing)
+    static constexpr bool DIRECT = NT == 3 && KTN == 8;
+    static constexpr size_t LDS = (size_t)(4 * KTN * NT * (DIRECT ? 1 : 2) + (DIRECT ? 18 : 36) + NCT * XCH) * GDN_FRAG * 2 + 2 * 3 * 64 * 4;
 };
 
 template <typename VT, int KTN, int NCT>
@@ -169,9 +48,9 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* sK = reinterpret_cast<uint16_t*>(smem);       // [4][KTN][NT]
     uint16_t* sQ = sK + 4 * KTN * NT * GDN_FRAG;
-    uint16_t* sT = sQ + 4 * KTN * NT * GDN_FRAG;                 // T'^T [6][3]
+    uint16_t* sT = sQ + (C::DIRECT ? 0 : 4 * KTN * NT * GDN_FRAG);   // T'^T [6][3]
     uint16_t* sP = sT + GDN_BLKS * 3 * GDN_FRAG;            // P^T
-    uint16_t* sX = sP + GDN_BLKS * 3 * GDN_FRAG;
+    uint16_t* sX = sP + (C::DIRECT ? 0 : GDN_BLKS * 3 * GDN_FRAG);
     float* sV = reinterpret_cast<float*>(sX + C::NCT * C::XCH * GDN_FRAG);   // [2][gamma, end, beta][64]
 
     const int groups = (a.dv + 16 * C::NCT - 1) / (16 * C::NCT);
@@ -208,7 +87,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
     float rV, rY[4][4];
     const auto fetch_kq = [&](int c) {
         rK.template fetch<KTN>(kp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
-        rQ.template fetch<KTN>(qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
+        if constexpr (!C::DIRECT) rQ.template fetch<KTN>(qp + (size_t)c * GDN_C * a.dk, w * C::FPW, len - c * GDN_C, a.dk);
         const int which = w == 0 ? GDN_V_GAM : w == 1 ? GDN_V_END : GDN_V_BETA;   // other waves repeat beta
         rV = a.vec[(ch0 + c) * GDN_VEC * 64 + which * 64 + lane];
     };
@@ -222,10 +101,23 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
         if constexpr (NW == 2) rB = a.vec[(ch0 + c) * GDN_VEC * 64 + GDN_V_BETA * 64 + lane];
     };
     const auto fetch_t = [&](int c) { gdn_fetch_turns<NW>(rT, a.tf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
-    const auto fetch_p = [&](int c) { gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w); };
+    const auto fetch_p = [&](int c) {
+        if constexpr (!C::DIRECT) gdn_fetch_turns<NW>(rP, a.pf + (ch0 + c) * 18 * GDN_FRAG, 18, w);
+    };
+    const auto stage_p = [&]() {
+        if constexpr (!C::DIRECT) gdn_stage_turns<NW>(sP, 18, w, rP);
+    };
+    const auto p_frag = [&](int c, int blk) {
+        if constexpr (C::DIRECT) return gdn_load_frag<3>(a.pf, (ch0 + c) * GDN_BLKS + blk);
+        else return gdn_load_frag<3>(sP, blk);
+    };
+    const auto q_turned = [&](int c, int dt, int kb) {
+        if constexpr (C::DIRECT) return gdn_load_frag<NT>(a.qt, (((size_t)(b * a.Hk + hk) * a.nC + c) * 2 * KTN + dt) * 2 + kb);
+        else return gdn_turned_frag<KTN, NT>(sQ, dt, kb);
+    };
     const auto stage_kq = [&](int par) {
         rK.stage(sK, w * C::FPW);
-        rQ.stage(sQ, w * C::FPW);
+        if constexpr (!C::DIRECT) rQ.stage(sQ, w * C::FPW);
         if (w < 3) sV[(par * 3 + w) * 64 + lane] = rV;
         if (NW == 2 && w == 0) sV[(par * 3 + 2) * 64 + lane] = rB;
     };
@@ -238,7 +130,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
         give_state();
         stage_kq((nc - 1) & 1);
         gdn_stage_turns<NW>(sT, 18, w, rT);
-        gdn_stage_turns<NW>(sP, 18, w, rP);
+        stage_p();
         const int c1 = max(nc - 2, 0);
         fetch_p(c1);
         fetch_t(c1);
@@ -274,12 +166,12 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
         if (h == 0) {
             const GdnFrag<3> y = gdn_stack(Y[0], Y[1]);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<3>(sP, gdn_up_blk(m, 0)), y, dE[m]);
+            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(p_frag(c, gdn_up_blk(m, 0)), y, dE[m]);
         }
         {
             const GdnFrag<3> y = gdn_stack(Y[2], Y[3]);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(gdn_load_frag<3>(sP, h ? 4 + m : 2 * m + 1), y, dE[m]);
+            for (int m = 0; m < 2; ++m) dE[m] = gdn_mm(p_frag(c, h ? 4 + m : 2 * m + 1), y, dE[m]);
         }
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
@@ -297,7 +189,7 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
         }
         const GdnFrag<3> y0 = gdn_stack(Y[0], Y[1]), y1 = gdn_stack(Y[2], Y[3]);
         __syncthreads();
-        gdn_stage_turns<NW>(sP, 18, w, rP);
+        stage_p();
         fetch_y(max(c - 1, 0));
         fetch_p(next);
         // dR = T'^T F
@@ -333,8 +225,8 @@ __global__ __launch_bounds__(2 * NCT * 64) void gdn_adjoint_halves_kernel(GdnArg
 #pragma unroll
             for (int d = 0; d < KTN; ++d) {
                 S[d] *= last;
-                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sQ, h * KTN + d, 0), y0, S[d]);
-                S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sQ, h * KTN + d, 1), y1, S[d]);
+                S[d] = gdn_mm(q_turned(c, h * KTN + d, 0), y0, S[d]);
+                S[d] = gdn_mm(q_turned(c, h * KTN + d, 1), y1, S[d]);
                 S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sK, h * KTN + d, h), nf, S[d]);
                 S[d] = gdn_mm(gdn_turned_frag<KTN, NT>(sK, h * KTN + d, 1 - h), no, S[d]);
             }
@@ -360,17 +252,12 @@ hipError_t launch_adjoint_tiles(const GdnArgs& a, hipStream_t st) {
 // column tiles to a workgroup as in the forward scan
 template <typename VT, int KTN>
 hipError_t launch_adjoint(const GdnArgs& a, hipStream_t st) {
-    if constexpr (KTN == 8 && sizeof(VT) == 4) {
-        gdn_adjoint_wide_kernel<<<dim3((a.dv + 63) / 64 * a.B * a.H), 256, 0, st>>>(a);
-        return hipGetLastError();
-    } else {
-        const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
-        if constexpr (KTN == 2 || (KTN == 4 && sizeof(VT) == 2)) {
-            if (tiles >= 4 * cus) return launch_adjoint_tiles<VT, KTN, 4>(a, st);
-            if (tiles >= 2 * cus) return launch_adjoint_tiles<VT, KTN, 2>(a, st);
-        }
-        return launch_adjoint_tiles<VT, KTN, 1>(a, st);
+    const int64_t tiles = (int64_t)((a.dv + 15) / 16) * a.B * a.H, cus = sdm_device_simds() / 4;
+    if constexpr (KTN == 2 || (KTN == 4 && sizeof(VT) == 2)) {
+        if (tiles >= 4 * cus) return launch_adjoint_tiles<VT, KTN, 4>(a, st);
+        if (tiles >= 2 * cus) return launch_adjoint_tiles<VT, KTN, 2>(a, st);
     }
+    return launch_adjoint_tiles<VT, KTN, 1>(a, st);
 }
 
 // ---------------------------------------------------------------- gradients

@@ -178,6 +178,7 @@ def test_padded_batch_leaves_rows_past_the_end(T):
 @pytest.mark.parametrize("B,Hk,H,T,dk,dv,start", [
     (1, 1, 1, 1, 4, 4, True), (1, 1, 2, 5, 32, 32, False), (2, 1, 3, 64, 36, 100, True), (1, 2, 2, 65, 128, 128, True),
     (1, 1, 1, 130, 64, 20, False), (1, 1, 2, 90, 256, 68, True), (2, 2, 6, 193, 72, 48, True),
+    (2, 2, 6, 260, 200, 48, True),
 ])
 def test_gradients(B, Hk, H, T, dk, dv, start, bf16):
     a, s0, dy, dS = inputs(B, Hk, H, T, dk, dv, bf16, start=start)
