@@ -298,9 +298,8 @@ def run(s):
         return dict(y=y, state=state, **{x: g[x] for x in ("dq", "dk", "dv", "dalpha", "dbeta", "dstate0")})
     if c["do"] == "forward":
         return dict(y=sdm.linear(s.x, s.w, s.bias, act=c["act"], residual=s.residual, heads=c["heads_out"]))
-    y, z, rest = sdm.linear(s.x, s.w, s.bias, act=c["act"], residual=s.residual, heads=c["heads_out"], want_z=True,
-                            want_rest=True)
-    g = sdm.linear_bwd(s.x, s.w, s.dy, z=z, z_rest=rest, act=c["act"], want_dbias=s.bias is not None)
+    y, z = sdm.linear(s.x, s.w, s.bias, act=c["act"], residual=s.residual, heads=c["heads_out"], want_z=True)
+    g = sdm.linear_bwd(s.x, s.w, s.dy, z=z, act=c["act"], want_dbias=s.bias is not None)
     return dict(y=y, z=z, **{x: g[x] for x in ("dx", "dw", "dbias") if g[x] is not None})
 
 
