@@ -740,6 +740,24 @@ def _check_linear(x, w):
     return B, T, K, N, heads
 
 
+class Preactivation(torch.Tensor):
+    """A bf16 pre-activation together with what its rounding left (`rest`, bf16), as linear(want_z=True) keeps it
+    for an activation's gradient.  To torch's functions it is the bf16 tensor, and what they return is a plain
+    one; widened (.float(), .double(), .to()) it is the value that was kept, the sum of both."""
+    __torch_function__ = torch._C._disabled_torch_function_impl
+    rest = None
+
+    def to(self, *args, **kwargs):
+        t = super().to(*args, **kwargs)
+        return t if self.rest is None or t.element_size() <= 2 else t + self.rest.to(t.device, t.dtype)
+
+    def float(self):
+        return self.to(torch.float32)
+
+    def double(self):
+        return self.to(torch.float64)
+
+
 def linear_workspace(x, w) -> torch.Tensor:
     B, T, K, N, _ = _check_linear(x, w)
     return _ws(lib().sdm_linear_workspace_bytes(_dtype_code(x), _dtype_code(w), B, T, K, N), x.device)
@@ -750,8 +768,9 @@ def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dty
     """A projection: z = x w^T + bias, y = act(z) + residual (act 0 identity, 1 SiLU, 2 GELU).  x [B,T,K] or
     head-major [B,heads,T,d] (K = heads d); w [N,K]; bias [N] fp32; residual [B,T,N] in y's dtype.  Returns y
     [B,T,N], or head-major [B,heads,T,N/heads] where heads > 0, in out_dtype (w's by default, or float32), and
-    z (laid out and typed as y) if wanted, and what a bf16 z's rounding left if that is wanted too (None of an
-    fp32 one).  An fp32 x with a bf16 w is rounded to bf16."""
+    z (laid out and typed as y) if wanted, for linear_bwd.  A bf16 z of an activation carries what its rounding
+    left (Preactivation); with want_rest that is returned as a tensor of its own beside a plain z (None of an fp32
+    one).  An fp32 x with a bf16 w is rounded to bf16."""
     B, T, K, N, x_heads = _check_linear(x, w)
     heads = int(heads)
     if heads < 0 or (heads and N % heads):
@@ -776,7 +795,7 @@ def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dty
     if y is None:
         y = torch.empty(shape, dtype=dt, device=dev)
     z = torch.empty_like(y) if want_z else None
-    rest = torch.empty_like(y) if want_rest and want_z and dt == torch.bfloat16 else None
+    rest = torch.empty_like(y) if want_z and (want_rest or act) and dt == torch.bfloat16 else None
     if workspace is None and need:
         workspace = _ws(need, dev)
     with _current(dev):
@@ -784,14 +803,23 @@ def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dty
                               _ptr(residual), B, T, K, N, heads, _ptr(y), _dtype_code(y), _ptr(z), _ptr(rest), _ptr(workspace),
                               0 if workspace is None else workspace.numel(), _stream(dev))
     _check("sdm_linear", rc)
-    return (y, z, rest) if want_z and want_rest else (y, z) if want_z else y
+    if not want_z:
+        return y
+    if want_rest:
+        return y, z, rest
+    if rest is not None:
+        z = z.as_subclass(Preactivation)
+        z.rest = rest
+    return y, z
 
 
 def linear_bwd(x, w, dy, z=None, act: int = 0, z_rest=None, want_dx: bool = True, want_dw: bool = True, want_dbias: bool = False,
                workspace=None):
     """Reverse mode of linear: dz = dy act'(z), dx = dz w, dw = dz^T x, dbias = sum dz (residual's gradient is
-    dy).  dy [B,T,N] or head-major [B,heads,T,N/heads], in w's dtype or float32; z (and z_rest) as linear
-    returned them (not needed with act 0; without z_rest the slope is taken at the rounded z).  Returns a dict of dx (as x), dw (as w) and dbias (fp32); None where not wanted."""
+    dy).  dy [B,T,N] or head-major [B,heads,T,N/heads], in w's dtype or float32; z as linear returned it (not
+    needed with act 0), with z_rest where that was returned beside it.  Returns a dict of dx (as x), dw (as w) and
+    dbias (fp32); None where not wanted.  A plain bf16 z has lost what an fp32 dbias needs, so that one is refused
+    without z_rest; z.float() takes the rounded values as they are."""
     B, T, K, N, x_heads = _check_linear(x, w)
     dB, dT, dN, heads = _tokens_of(dy, "dy")
     if (dB, dT, dN) != (B, T, N):
@@ -802,6 +830,10 @@ def linear_bwd(x, w, dy, z=None, act: int = 0, z_rest=None, want_dx: bool = True
         raise ValueError("z is required for an activation's gradient")
     if z is not None:
         _expect(z, "z", tuple(dy.shape), (w.dtype, torch.float32))
+        if z_rest is None and isinstance(z, Preactivation):
+            z_rest = z.rest
+        if act and want_dbias and z_rest is None and z.dtype == torch.bfloat16:
+            raise ValueError("dbias at a bf16 z needs what its rounding left: z as linear returned it, z_rest, or z.float()")
     if z_rest is not None:
         if z is None:
             raise ValueError("z_rest goes with z")
