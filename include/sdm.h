@@ -464,8 +464,9 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *   x         [B, T, K], or head-major [B, x_heads, T, K / x_heads] where
  *             x_heads > 0 (feature h (K / x_heads) + c is head h's value c), in x_dtype.
  *   w         [N, K] in w_dtype.  Types: both fp32, both bf16, or an fp32 x
- *             with a bf16 w: x is then rounded to bf16 as it is read (the
- *             epilogue's rows, which sdm_norm_gate leaves in fp32).
+ *             with a bf16 w (the epilogue's rows, which sdm_norm_gate leaves in
+ *             fp32): x then enters in full for an fp32 y, to 2^-15 for a bf16 one.
+ *             A caller who wants it rounded, at a third to a half of the work, rounds it.
  *   bias      [N] fp32 or NULL;  act  0 identity, 1 SiLU, 2 GELU (erf form).
  *   residual  [B, T, N] in y_dtype or NULL; only with y_heads = 0.
  *   y         out [B, T, N], or head-major [B, y_heads, T, N / y_heads] as the
@@ -474,8 +475,8 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *             out beside a bf16 z: what its rounding left, in bf16.
  * Sums are fp32; bf16 products are exact, fp32 ones fp32.  Sums over split
  * depths are added in a fixed order: results are the same from run to run.
- * y may be residual; no other output may overlap an input.  An infinite fp32 factor of
- * fp32 products counts as NaN; a token's stay in its own outputs.
+ * y may be residual; no other output may overlap an input.  An infinite fp32 factor
+ * counts as NaN; a token's stay in its own outputs.
  *   workspace  at least sdm_linear_workspace_bytes() bytes, 256-B aligned;
  *              NULL where that is 0.
  * Limits: K and K / x_heads multiples of 8 (bf16 w) or 4 (fp32); B T <= 2^26;

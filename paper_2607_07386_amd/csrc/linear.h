@@ -28,9 +28,10 @@ struct LinGemm {
     LinMat a, b;
     bool ta, tb;
     int I, J, R;          // output rows, output columns, depth
-    // 1, or 6: a and b hold three bf16 parts of fp32 values, `plane` values apart, and the
-    // products of parts of total order <= 2 are added up
+    // a factor's fp32 values stand as two or three bf16 parts, `plane` values apart; `combos` products of
+    // parts are added up, the c-th of parts (part_a >> 2c) & 3 and (part_b >> 2c) & 3 (lin_products)
     int combos;
+    uint32_t part_a, part_b;
     int64_t plane_a, plane_b;
     // out = act(C + bias) + residual, pre = C + bias, rest = what pre's rounding to bf16 left; all laid out
     // and typed as `out`
@@ -45,6 +46,20 @@ struct LinGemm {
     bool big;             // 256 x 256 tiles, else 128 x 128
     float* part;
 };
+
+// The products of parts of total order <= `order` of a factor of na parts and one of nb, smallest first.
+inline void lin_products(LinGemm& g, int na, int nb, int order) {
+    g.combos = 0;
+    g.part_a = g.part_b = 0;
+    for (int o = order; o >= 0; --o)
+        for (int i = 0; i < na; ++i) {
+            const int j = o - i;
+            if (j < 0 || j >= nb) continue;
+            g.part_a |= (uint32_t)i << 2 * g.combos;
+            g.part_b |= (uint32_t)j << 2 * g.combos;
+            ++g.combos;
+        }
+}
 
 #define LIN_UP8(x) (((x) + 7) / 8 * 8)
 struct LinPlan {
@@ -61,7 +76,8 @@ hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st);
 #define LIN_SKINNY 64
 inline bool lin_skinny(int I, int J, bool x_f32) { return I <= LIN_SKINNY || J <= (x_f32 ? LIN_SKINNY : LIN_SKINNY / 2); }
 hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st);
-// an fp32 matrix as np bf16 planes [rows][ld] (np 1: rounded, 3: the parts), zeros past its end
+// an fp32 matrix as np bf16 planes [rows][ld] (np 1: rounded, 2: and what that leaves, to 2^-15, 3: to 2^-24),
+// zeros past its end
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st);
 // dz = dy act'(z) as np planes [rows][ld], zeros past M and N, and dbias = its column sums
 // (through parts [sdm_linear_dz_parts(rows, ld)][N] added in order).  dz and rest may be NULL.

@@ -326,10 +326,8 @@ __global__ __launch_bounds__(WR* WC * 64) void linear_tile_kernel(LinGemm g, int
     ta.init(g.a, i0);
     tb.init(g.b, j0);
     const auto fetch = [&](int s, unsigned char* la, unsigned char* lb) {
-        // fp32 factors: the products of parts of total order <= 2, smallest first
-        // (parts (0,2) (1,1) (2,0) (0,1) (1,0) (0,0), two bits each)
-        const int c = g.combos > 1 ? s / depth : 5, r0 = (g.combos > 1 ? s - c * depth : s) * BK;
-        const int pa = (0x124 >> 2 * c) & 3, pb = (0x46 >> 2 * c) & 3;
+        const int c = g.combos > 1 ? s / depth : 0, r0 = (g.combos > 1 ? s - c * depth : s) * BK;
+        const int pa = (g.part_a >> 2 * c) & 3, pb = (g.part_b >> 2 * c) & 3;
         ta.fetch(g.a, i0, r0, pa * g.plane_a, la);
         tb.fetch(g.b, j0, r0, pb * g.plane_b, lb);
     };
@@ -442,25 +440,16 @@ bool even_depth(const LinMat& m, bool tr, int R) {
 // outputs: 21 us (3.2 TB/s), fp32 35 us (3.9 TB/s).
 // eight depths of a row, from offsets o0 and o1 (the second four, which may be another
 // head's); zeros where the depth has ended
-template <int NT>
-__device__ __forceinline__ GdnFrag<NT> skinny_frag(const float* row, int64_t o0, int64_t o1, bool ok0, bool ok1) {
+__device__ __forceinline__ GdnFrag<3> skinny_frag(const float* row, int64_t o0, int64_t o1, bool ok0, bool ok1) {
     const v4f a = v4sel(ok0, ld4(row + o0), v4zero()), b = v4sel(ok1, ld4(row + o1), v4zero());
     const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-    if constexpr (NT == 3) {
-        return gdn_split(x);
-    } else {
-        GdnFrag<1> f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f.t[0][i] = (__bf16)x[i];
-        return f;
-    }
+    return gdn_split(x);
 }
-template <int NT>
-__device__ __forceinline__ GdnFrag<NT> skinny_frag(const bf16_t* row, int64_t o0, int64_t, bool ok0, bool) {
+__device__ __forceinline__ GdnFrag<1> skinny_frag(const bf16_t* row, int64_t o0, int64_t, bool ok0, bool) {
     u4v v = *reinterpret_cast<const u4v*>(row + o0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = ok0 ? v[i] : 0u;
-    GdnFrag<NT> f;
+    GdnFrag<1> f;
     f.t[0] = __builtin_bit_cast(sdm_bf16x8, v);
     return f;
 }
@@ -469,7 +458,6 @@ __device__ __forceinline__ GdnFrag<NT> skinny_frag(const bf16_t* row, int64_t o0
 // X_MANY: the factor with many rows is x.
 template <typename BT, typename ST, int MT, bool X_FLAT, bool X_MANY>
 __global__ __launch_bounds__(512) void linear_skinny_kernel(LinGemm g) {
-    constexpr int NT = sizeof(BT) == 4 && sizeof(ST) == 4 ? 3 : 1;
     __shared__ float red[8][MT][256];
     const LinMat &big = X_MANY ? g.a : g.b, &few = X_MANY ? g.b : g.a;
     const int nb = X_MANY ? g.I : g.J, nf = X_MANY ? g.J : g.I;
@@ -489,10 +477,10 @@ __global__ __launch_bounds__(512) void linear_skinny_kernel(LinGemm g) {
             const bool ok0 = k < g.R, ok1 = k + 4 < g.R;
             const int ka = ok0 ? k : 0, kb = ok1 ? k + 4 : 0;
             const int64_t xa = X_FLAT ? ka : mat_col(g.a, ka), xb = X_FLAT ? kb : mat_col(g.a, kb);
-            const GdnFrag<NT> fb = skinny_frag<NT>(bp, X_MANY ? xa : ka, X_MANY ? xb : kb, ok0, ok1);
+            const auto fb = skinny_frag(bp, X_MANY ? xa : ka, X_MANY ? xb : kb, ok0, ok1);
 #pragma unroll
             for (int m = 0; m < MT; ++m)
-                acc[m] = gdn_mm(skinny_frag<NT>(fp[m], X_MANY ? ka : xa, X_MANY ? kb : xb, ok0, ok1), fb, acc[m]);
+                acc[m] = gdn_mm(skinny_frag(fp[m], X_MANY ? ka : xa, X_MANY ? kb : xb, ok0, ok1), fb, acc[m]);
         }
     }
 #pragma unroll
@@ -589,11 +577,21 @@ __global__ __launch_bounds__(256) void linear_dw_few_kernel(LinMat x, const bf16
 }
 
 // ---------------------------------------------------------------- parts, dz, dbias
-// NP = 1: rounded to bf16; NP = 3: the three bf16 parts of an fp32 value.
+// NP = 1: rounded to bf16; NP = 2: its top 16 bits and what they leave, rounded; NP = 3: the
+// three bf16 parts of an fp32 value.
 template <int NP>
 __device__ __forceinline__ void put_parts(bf16_t* p, int64_t plane, const float (&x)[8]) {
     if constexpr (NP == 1) {
         st8(p, SDM_DT_BF16, 0, x);
+    } else if constexpr (NP == 2) {
+        float hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            hi[i] = __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
+            lo[i] = x[i] - hi[i];
+        }
+        st8(p, SDM_DT_BF16, 0, hi);
+        st8(p + plane, SDM_DT_BF16, 0, lo);
     } else {
         const GdnFrag<3> f = gdn_split(x);
 #pragma unroll
@@ -767,6 +765,7 @@ hipError_t sdm_launch_linear_dw_few(const LinMat& x, const void* dz, int64_t pla
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st) {
     const dim3 grid((ld + 255) / 256, std::min((rows + 7) / 8, 2048));
     if (np == 3) linear_parts_kernel<3><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
+    else if (np == 2) linear_parts_kernel<2><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
     else linear_parts_kernel<1><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
     return hipGetLastError();
 }

@@ -51,9 +51,13 @@ const char* too_large(int B, int T, int K, int N) {
 }
 
 int up64(int x) { return (x + 63) / 64 * 64; }
-int parts_of(int w_dtype) { return w_dtype == SDM_F32 ? 3 : 1; }
-int combos_of(int w_dtype) { return w_dtype == SDM_F32 ? 6 : 1; }
-int steps_of(int R, int w_dtype) { return (R + 63) / 64 * combos_of(w_dtype); }
+int parts_of(int dtype) { return dtype == SDM_F32 ? 3 : 1; }
+// Parts of x in the forward.  Two keep 2^-15 of an fp32 x, a 128th of what the rounding of a bf16
+// result takes off; an fp32 result gets all three, and so does any with an fp32 w.
+int x_parts(int x_dtype, int w_dtype, int y_dtype) {
+    return x_dtype == SDM_BF16 ? 1 : w_dtype == SDM_F32 || y_dtype == SDM_F32 ? 3 : 2;
+}
+int steps_of(int R, int combos) { return (R + 63) / 64 * combos; }
 
 // Offsets into a call's workspace.  fp32 factors enter the products as bf16 planes,
 // padded to multiples of 64 both ways.
@@ -71,12 +75,13 @@ struct Ws {
 size_t planes(int np, int rows, int cols) { return (size_t)np * up64(rows) * up64(cols) * 2; }
 size_t split_bytes(const LinPlan& p, int I, int J) { return p.split > 1 ? (size_t)p.split * I * LIN_UP8(J) * 4 : 0; }
 
-Ws fwd_ws(int x_dtype, int w_dtype, int M, int K, int N) {
+Ws fwd_ws(int x_dtype, int w_dtype, int y_dtype, int M, int K, int N) {
     Ws s;
     if (lin_skinny(M, N, x_dtype == SDM_F32)) return s;
-    if (x_dtype == SDM_F32) s.x = s.take(planes(parts_of(w_dtype), M, K));
+    const int np = x_parts(x_dtype, w_dtype, y_dtype);
+    if (x_dtype == SDM_F32) s.x = s.take(planes(np, M, K));
     if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
-    s.py = sdm_linear_plan(M, N, steps_of(K, w_dtype));
+    s.py = sdm_linear_plan(M, N, steps_of(K, w_dtype == SDM_F32 ? 6 : np));
     s.split = s.take(split_bytes(s.py, M, N));
     return s;
 }
@@ -89,8 +94,9 @@ Ws bwd_ws(int x_dtype, int w_dtype, int act, int dy_dtype, int y_heads, int M, i
     if (x_dtype == SDM_F32 && !s.few) s.x = s.take(planes(np, M, K));
     if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
     s.parts = s.take((size_t)sdm_linear_dz_parts(up64(M), up64(N)) * N * 4);
-    s.px = sdm_linear_plan(M, K, steps_of(N, w_dtype));
-    s.pw = sdm_linear_plan(N, K, steps_of(M, w_dtype));
+    const int combos = w_dtype == SDM_F32 ? 6 : 1;
+    s.px = sdm_linear_plan(M, K, steps_of(N, combos));
+    s.pw = sdm_linear_plan(N, K, steps_of(M, combos));
     if (s.few) s.pw.split = sdm_linear_dw_few_split(M, K);
     const size_t dw_bytes = s.few ? (size_t)s.pw.split * N * LIN_UP8(K) * 4 : split_bytes(s.pw, N, K);
     s.split = s.take(std::max(split_bytes(s.px, M, K), dw_bytes));
@@ -109,7 +115,9 @@ extern "C" {
 
 size_t sdm_linear_workspace_bytes(int x_dtype, int w_dtype, int B, int T, int K, int N) {
     if (bad_sizes(x_dtype, 0, w_dtype, 0, B, T, K, N, 0) || too_large(B, T, K, N) || (int64_t)B * T == 0) return 0;
-    return fwd_ws(x_dtype, w_dtype, B * T, K, N).total;
+    // for either type of y: a depth of more parts may be split otherwise
+    return std::max(fwd_ws(x_dtype, w_dtype, SDM_F32, B * T, K, N).total,
+                    fwd_ws(x_dtype, w_dtype, w_dtype, B * T, K, N).total);
 }
 
 int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dtype, const float* bias, int act,
@@ -140,7 +148,7 @@ int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dty
     g.I = M;
     g.J = N;
     g.R = K;
-    g.combos = combos_of(w_dtype);
+    lin_products(g, x_parts(x_dtype, w_dtype, y_dtype), parts_of(w_dtype), 2);
     g.out = lin_tokens(y, y_dtype, B, T, N, y_heads);
     g.pre = z;
     g.rest = z_rest;
@@ -154,9 +162,9 @@ int sdm_linear(const void* x, int x_dtype, int x_heads, const void* w, int w_dty
         e = sdm_launch_linear_skinny(g, st);
         return e == hipSuccess ? SDM_OK : hip_fail(e, "sdm_linear launch");
     }
-    const Ws L = fwd_ws(x_dtype, w_dtype, M, K, N);
+    const Ws L = fwd_ws(x_dtype, w_dtype, y_dtype, M, K, N);
     if (x_dtype == SDM_F32) {
-        e = sdm_launch_linear_parts(g.a, parts_of(w_dtype), up64(M), up64(K), ws + L.x, st);
+        e = sdm_launch_linear_parts(g.a, x_parts(x_dtype, w_dtype, y_dtype), up64(M), up64(K), ws + L.x, st);
         g.a = plane_mat(ws + L.x, M, K, false);
         g.plane_a = plane_len(M, K);
     }
@@ -215,7 +223,7 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
         e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_rest, z_dtype, act, np, up64(M), up64(N),
                                  L.direct ? nullptr : ws + L.dz, reinterpret_cast<float*>(ws + L.parts), dbias, st);
     LinGemm g{};
-    g.combos = combos_of(w_dtype);
+    lin_products(g, np, np, 2);
     g.tb = true;
     g.part = reinterpret_cast<float*>(ws + L.split);
     g.plane_a = plane_len(M, N);

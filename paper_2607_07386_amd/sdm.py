@@ -770,7 +770,7 @@ def linear(x, w, bias=None, act: int = 0, residual=None, heads: int = 0, out_dty
     [B,T,N], or head-major [B,heads,T,N/heads] where heads > 0, in out_dtype (w's by default, or float32), and
     z (laid out and typed as y) if wanted, for linear_bwd.  A bf16 z of an activation carries what its rounding
     left (Preactivation); with want_rest that is returned as a tensor of its own beside a plain z (None of an fp32
-    one).  An fp32 x with a bf16 w is rounded to bf16."""
+    one).  An fp32 x enters in full beside a bf16 w too (x.bfloat16() is the rounded product)."""
     B, T, K, N, x_heads = _check_linear(x, w)
     heads = int(heads)
     if heads < 0 or (heads and N % heads):

@@ -1,8 +1,11 @@
-"""How many bits the projections keep: the bias's gradient of the plain training call.
+"""How many bits the projections keep: the bias's gradient of the plain training call, fp32 rows beside bf16 weights.
 
 Tolerances count half steps (bf16 2^-8, fp32 2^-24).  A kept bf16 pre-activation with what its rounding left is off by
 2^-16 of itself; |z act''(z)| < 1 for both activations, so a term of dbias is off by 2^-16 of dy at most, and their sum,
-whose terms have either sign, by 2^-16 of its largest value and by the fp32 additions' sqrt(M) 2^-24."""
+whose terms have either sign, by 2^-16 of its largest value and by the fp32 additions' sqrt(M) 2^-24.  A product of fp32
+parts leaves out terms of order 3 and above: the parts are cut, so each is below 2^-7 of the one before, and what is
+left out below 2^-20 of the term; the sum of K terms adds sqrt(K) 2^-24 (roundings either way).  Two parts leave
+2^-15 of a term.  A bf16 result is one half step off on top."""
 import pytest
 import torch
 
@@ -11,6 +14,12 @@ from tests.gpu_util import DEV
 from tests.test_gpu_linear import ACTS, case, close, flat, reference
 
 pytestmark = pytest.mark.gpu
+
+HALF_BF16 = 2.0 ** -8
+
+
+def f32_tol(depth):
+    return 2.0 ** -20 + depth ** 0.5 * 2.0 ** -24
 
 
 def definition_gradients(x, w, bias, dy, act, hin, hout):
@@ -46,3 +55,23 @@ def test_bias_gradient_of_the_plain_call(shape, kind, act):
     for name in g:
         assert torch.equal(g[name], g2[name]), name
 
+
+MIXED = [  # B, T, K, N, heads in, heads out: few rows, few outputs, tiles, odd sizes, a split depth
+    (3, 1, 64, 40, 4, 0), (16, 1, 256, 512, 0, 4), (2, 200, 136, 24, 0, 0), (2, 257, 96, 96, 2, 3), (1, 300, 704, 260, 0, 0),
+    (3, 50, 520, 90, 13, 0), (1, 640, 512, 512, 8, 8), (1, 129, 4096, 130, 0, 0),
+]
+
+
+@pytest.mark.parametrize("shape", MIXED)
+def test_fp32_rows_beside_bf16_weights(shape):
+    """An fp32 x enters in full: an fp32 result to fp32's accuracy, a bf16 one off by its own rounding."""
+    B, T, K, N, hin, hout = shape
+    x, w, bias, _, _ = case(B, T, K, N, hin, hout, True, x_f32=True)
+    ry, _ = reference(x.double(), w.double(), bias.double(), 0, None, hout)
+    y, z = sdm.linear(x, w, bias, heads=hout, out_dtype=torch.float32, want_z=True)
+    close(y, ry, "y in fp32", f32_tol(K))
+    assert torch.equal(y, z)
+    y = sdm.linear(x, w, bias, heads=hout)
+    size, _ = reference(x.double().abs(), w.double().abs(), bias.double().abs(), 0, None, hout)
+    over = (y.double() - ry).abs() - HALF_BF16 * ry.abs() - 2.0 ** -14 * size / K ** 0.5
+    assert over.max() <= 0, f"a bf16 result is off by more than its rounding: {over.max():.2e}"
