@@ -466,7 +466,7 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *   w         [N, K] in w_dtype.  Types: both fp32, both bf16, or an fp32 x
  *             with a bf16 w (the epilogue's rows, which sdm_norm_gate leaves in
  *             fp32): x then enters in full for an fp32 y, to 2^-15 for a bf16 one.
- *             A caller who wants it rounded, at a third to a half of the work, rounds it.
+ *             A caller who wants the rounded product, less work, rounds x.
  *   bias      [N] fp32 or NULL;  act  0 identity, 1 SiLU, 2 GELU (erf form).
  *   residual  [B, T, N] in y_dtype or NULL; only with y_heads = 0.
  *   y         out [B, T, N], or head-major [B, y_heads, T, N / y_heads] as the
@@ -486,11 +486,13 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *   dx = dz W,  dw = dz^T x,  dbias[n] = sum over tokens of dz;  the gradient of
  *   residual is dy itself.
  *   dy        laid out as y, in dy_dtype: w's type, or fp32 (as the recurrences'
- *             backwards write their gradients).  dz is rounded to w's type, in which
- *             it enters the products; dbias sums it in fp32 before that.
+ *             backwards write their gradients).  dbias sums dz in fp32.  With fp32 x or w
+ *             dz enters the products in full; else, with an fp32 dy, to 2^-15 (dx and dw are
+ *             bf16); with a bf16 dy it is rounded to bf16.  An fp32 x beside a bf16 w enters
+ *             dw to 2^-15.
  *   z, z_rest as sdm_linear wrote them (z_dtype); NULL with act 0.  With z_rest the
- *             activation's slope is taken at z to 2^-17; without it at the rounded z, whose
- *             2^-9 shows in dbias (the products round dz to bf16 anyway).
+ *             activation's slope is taken at z to 2^-16; without it at the rounded z, whose
+ *             2^-8 shows in dbias.
  *   dx        optional out, laid out and typed as x;  dw  optional out [N, K] in
  *             w_dtype;  dbias  optional out [N] fp32.
  *   workspace  at least sdm_linear_bwd_workspace_bytes() bytes, 256-B aligned.

@@ -76,10 +76,9 @@ hipError_t sdm_launch_linear(const LinGemm& g, hipStream_t st);
 #define LIN_SKINNY 64
 inline bool lin_skinny(int I, int J, bool x_f32) { return I <= LIN_SKINNY || J <= (x_f32 ? LIN_SKINNY : LIN_SKINNY / 2); }
 hipError_t sdm_launch_linear_skinny(const LinGemm& g, hipStream_t st);
-// an fp32 matrix as np bf16 planes [rows][ld] (np 1: rounded, 2: and what that leaves, to 2^-15, 3: to 2^-24),
-// zeros past its end
+// an fp32 matrix as np bf16 planes [rows][ld] (2: to 2^-15 of a value, 3: to 2^-24), zeros past its end
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st);
-// dz = dy act'(z) as np planes [rows][ld], zeros past M and N, and dbias = its column sums
+// dz = dy act'(z) as np planes [rows][ld] (1: rounded), zeros past M and N, and dbias = its column sums
 // (through parts [sdm_linear_dz_parts(rows, ld)][N] added in order).  dz and rest may be NULL.
 int sdm_linear_dz_parts(int rows, int ld);
 hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, const void* rest, int z_dtype, int act, int np, int rows, int ld,

@@ -765,8 +765,7 @@ hipError_t sdm_launch_linear_dw_few(const LinMat& x, const void* dz, int64_t pla
 hipError_t sdm_launch_linear_parts(const LinMat& m, int np, int rows, int ld, void* out, hipStream_t st) {
     const dim3 grid((ld + 255) / 256, std::min((rows + 7) / 8, 2048));
     if (np == 3) linear_parts_kernel<3><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
-    else if (np == 2) linear_parts_kernel<2><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
-    else linear_parts_kernel<1><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
+    else linear_parts_kernel<2><<<grid, 256, 0, st>>>(m, rows, ld, static_cast<bf16_t*>(out), (int64_t)rows * ld);
     return hipGetLastError();
 }
 
@@ -787,6 +786,7 @@ hipError_t sdm_launch_linear_dz(const LinMat& dy, const void* z, const void* res
     bf16_t* o = static_cast<bf16_t*>(dz);
     const int64_t plane = (int64_t)rows * ld;
     if (np == 3) linear_dz_kernel<3><<<grid, 256, 0, st>>>(dy, z, rest, z_dtype, act, rows, per, ld, o, plane, p);
+    else if (np == 2) linear_dz_kernel<2><<<grid, 256, 0, st>>>(dy, z, rest, z_dtype, act, rows, per, ld, o, plane, p);
     else linear_dz_kernel<1><<<grid, 256, 0, st>>>(dy, z, rest, z_dtype, act, rows, per, ld, o, plane, p);
     if (dbias) linear_colsum_kernel<<<(dy.cols + 31) / 32, 1024, 0, st>>>(part, parts, dy.cols, dbias);
     return hipGetLastError();

@@ -53,9 +53,23 @@ const char* too_large(int B, int T, int K, int N) {
 int up64(int x) { return (x + 63) / 64 * 64; }
 int parts_of(int dtype) { return dtype == SDM_F32 ? 3 : 1; }
 // Parts of x in the forward.  Two keep 2^-15 of an fp32 x, a 128th of what the rounding of a bf16
-// result takes off; an fp32 result gets all three, and so does any with an fp32 w.
+// result takes off; an fp32 result gets all three, and so does any with an fp32 w.  16,384 x 2048 head-major by
+// 2048 with a residual: 305 to 313 us, 192 where the caller rounds x, that pass included; an fp32 result 418.
 int x_parts(int x_dtype, int w_dtype, int y_dtype) {
     return x_dtype == SDM_BF16 ? 1 : w_dtype == SDM_F32 || y_dtype == SDM_F32 ? 3 : 2;
+}
+// Parts of dz in the backward: all three for fp32 gradients (of an fp32 x, an fp32 w), two for an fp32 dy where the
+// gradients are bf16.  From a bf16 dy an activation's dz is rounded to bf16, as a program that holds its
+// activations' gradients in bf16 has it: two parts double both products (16,384 x 2048 x 2048 with dbias:
+// 353 us, 596 from an fp32 dy) for dx and dw that are rounded to 2^-8 themselves; without an activation it is exact.
+int dz_parts(int x_dtype, int w_dtype, int act, int dy_dtype) {
+    if (w_dtype == SDM_F32) return 3;
+    if (act == 0 && dy_dtype == SDM_BF16) return 1;
+    return x_dtype == SDM_F32 ? 3 : dy_dtype == SDM_F32 ? 2 : 1;
+}
+// the products of dw = dz^T x: to order 2 for an fp32 dw, to order 1 for a bf16 one
+void dw_products(LinGemm& g, int x_dtype, int w_dtype, int nz) {
+    lin_products(g, nz, w_dtype == SDM_F32 ? 3 : x_dtype == SDM_F32 ? 2 : 1, w_dtype == SDM_F32 ? 2 : 1);
 }
 int steps_of(int R, int combos) { return (R + 63) / 64 * combos; }
 
@@ -87,16 +101,18 @@ Ws fwd_ws(int x_dtype, int w_dtype, int y_dtype, int M, int K, int N) {
 }
 Ws bwd_ws(int x_dtype, int w_dtype, int act, int dy_dtype, int y_heads, int M, int K, int N) {
     Ws s;
-    const int np = parts_of(w_dtype);
+    const int nz = dz_parts(x_dtype, w_dtype, act, dy_dtype);
     s.direct = w_dtype == SDM_BF16 && act == 0 && dy_dtype == SDM_BF16 && y_heads == 0 && N % 8 == 0;
-    if (!s.direct) s.dz = s.take(planes(np, M, N));
+    if (!s.direct) s.dz = s.take(planes(nz, M, N));
     s.few = w_dtype == SDM_F32 && N <= LIN_SKINNY;
-    if (x_dtype == SDM_F32 && !s.few) s.x = s.take(planes(np, M, K));
+    if (x_dtype == SDM_F32 && !s.few) s.x = s.take(planes(w_dtype == SDM_F32 ? 3 : 2, M, K));
     if (w_dtype == SDM_F32) s.w = s.take(planes(3, N, K));
     s.parts = s.take((size_t)sdm_linear_dz_parts(up64(M), up64(N)) * N * 4);
-    const int combos = w_dtype == SDM_F32 ? 6 : 1;
-    s.px = sdm_linear_plan(M, K, steps_of(N, combos));
-    s.pw = sdm_linear_plan(N, K, steps_of(M, combos));
+    LinGemm g{};
+    lin_products(g, nz, parts_of(w_dtype), 2);
+    s.px = sdm_linear_plan(M, K, steps_of(N, g.combos));
+    dw_products(g, x_dtype, w_dtype, nz);
+    s.pw = sdm_linear_plan(N, K, steps_of(M, g.combos));
     if (s.few) s.pw.split = sdm_linear_dw_few_split(M, K);
     const size_t dw_bytes = s.few ? (size_t)s.pw.split * N * LIN_UP8(K) * 4 : split_bytes(s.pw, N, K);
     s.split = s.take(std::max(split_bytes(s.px, M, K), dw_bytes));
@@ -217,13 +233,13 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
     const int rc = check_ws(workspace, ws_bytes, L.total);
     if (rc != SDM_OK) return rc;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
-    const int np = parts_of(w_dtype);
+    const int nz = dz_parts(x_dtype, w_dtype, act, dy_dtype);
     SdmProfScope ps(SDM_K_LINEAR, st);
     if (!L.direct || dbias)
-        e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_rest, z_dtype, act, np, up64(M), up64(N),
+        e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_rest, z_dtype, act, nz, up64(M), up64(N),
                                  L.direct ? nullptr : ws + L.dz, reinterpret_cast<float*>(ws + L.parts), dbias, st);
     LinGemm g{};
-    lin_products(g, np, np, 2);
+    lin_products(g, nz, parts_of(w_dtype), 2);
     g.tb = true;
     g.part = reinterpret_cast<float*>(ws + L.split);
     g.plane_a = plane_len(M, N);
@@ -246,9 +262,10 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
     if (e == hipSuccess && dw) {
         g.a = L.direct ? lin_flat(dy, SDM_BF16, M, N, N) : plane_mat(ws + L.dz, M, N, true);
         g.ta = true;
+        dw_products(g, x_dtype, w_dtype, nz);
         g.b = lin_tokens(x, x_dtype, B, T, K, x_heads);
         if (x_dtype == SDM_F32 && !L.few) {
-            e = sdm_launch_linear_parts(g.b, np, up64(M), up64(K), ws + L.x, st);
+            e = sdm_launch_linear_parts(g.b, w_dtype == SDM_F32 ? 3 : 2, up64(M), up64(K), ws + L.x, st);
             g.b = plane_mat(ws + L.x, M, K, true);
             g.plane_b = plane_len(M, K);
         }

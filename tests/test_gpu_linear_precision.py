@@ -1,4 +1,4 @@
-"""How many bits the projections keep: the bias's gradient of the plain training call, fp32 rows beside bf16 weights.
+"""How many bits the projections keep: the bias's gradient of the plain training call, fp32 operands beside bf16 ones.
 
 Tolerances count half steps (bf16 2^-8, fp32 2^-24).  A kept bf16 pre-activation with what its rounding left is off by
 2^-16 of itself; |z act''(z)| < 1 for both activations, so a term of dbias is off by 2^-16 of dy at most, and their sum,
@@ -75,3 +75,27 @@ def test_fp32_rows_beside_bf16_weights(shape):
     size, _ = reference(x.double().abs(), w.double().abs(), bias.double().abs(), 0, None, hout)
     over = (y.double() - ry).abs() - HALF_BF16 * ry.abs() - 2.0 ** -14 * size / K ** 0.5
     assert over.max() <= 0, f"a bf16 result is off by more than its rounding: {over.max():.2e}"
+
+
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("x_f32,dy_f32", [(True, False), (True, True), (False, True)])
+@pytest.mark.parametrize("shape", MIXED)
+def test_gradients_of_fp32_rows_beside_bf16_weights(shape, x_f32, dy_f32, act):
+    """An fp32 x or dy enters the gradients with more bits than a bf16 result keeps; an fp32 dx is one of fp32's accuracy."""
+    B, T, K, N, hin, hout = shape
+    x, w, bias, _, dy = case(B, T, K, N, hin, hout, True, x_f32=x_f32)
+    dy = dy.float() * 1.001 if dy_f32 else dy
+    z = None
+    if act:
+        _, z = sdm.linear(x, w, bias, act=act, heads=hout, want_z=True)
+    g = sdm.linear_bwd(x, w, dy, z=z, act=act, want_dbias=True)
+    dx, dw, dbias, _ = definition_gradients(x, w, bias, dy, act, hin, hout)
+    # the slope's own place (the kept z, and an fp32 x that entered it in two parts), then the activation's roundings
+    at_z = (2.0 ** -16 + (2.0 ** -15 if x_f32 else 0.0) + 2.0 ** -20) if act else 0.0
+    close(g["dbias"], dbias, "dbias", at_z + 2.0 ** -24 + (B * T) ** 0.5 * 2.0 ** -24)
+    if x_f32:
+        close(g["dx"], dx, "dx", at_z + f32_tol(N))
+    # two cut parts leave 2^-14 of a term, in a sum of either sign of its root mean square
+    for name, ref in (("dw", dw),) if x_f32 else (("dx", dx), ("dw", dw)):
+        over = (g[name].double() - ref).abs() - HALF_BF16 * ref.abs() - 2.0 ** -11 * ref.square().mean().sqrt()
+        assert over.max() <= 0, f"{name} is off by more than its rounding: {over.max():.2e}"
