@@ -237,7 +237,7 @@ int sdm_linear_bwd(const void* x, int x_dtype, int x_heads, const void* w, int w
     SdmProfScope ps(SDM_K_LINEAR, st);
     if (!L.direct || dbias)
         e = sdm_launch_linear_dz(lin_tokens(dy, dy_dtype, B, T, N, y_heads), z, z_rest, z_dtype, act, nz, up64(M), up64(N),
-                                 L.direct ? nullptr : ws + L.dz, reinterpret_cast<float*>(ws + L.parts), dbias, st);
+                                 L.direct || !(dx || dw) ? nullptr : ws + L.dz, reinterpret_cast<float*>(ws + L.parts), dbias, st);
     LinGemm g{};
     lin_products(g, nz, parts_of(w_dtype), 2);
     g.tb = true;

@@ -99,3 +99,17 @@ def test_gradients_of_fp32_rows_beside_bf16_weights(shape, x_f32, dy_f32, act):
     for name, ref in (("dw", dw),) if x_f32 else (("dx", dx), ("dw", dw)):
         over = (g[name].double() - ref).abs() - HALF_BF16 * ref.abs() - 2.0 ** -11 * ref.square().mean().sqrt()
         assert over.max() <= 0, f"{name} is off by more than its rounding: {over.max():.2e}"
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_bias_gradient_alone_writes_no_dz(bf16):
+    """With neither dx nor dw wanted, dz's planes at the workspace's start are left as they were."""
+    x, w, bias, _, dy = case(2, 300, 64, 96, 0, 6, bf16)
+    _, z = sdm.linear(x, w, bias, act=1, heads=6, want_z=True)
+    code = int(bf16)
+    ws = torch.full((sdm.lib().sdm_linear_bwd_workspace_bytes(code, code, 1, code, 2, 300, 64, 96, 6),), 0xA5,
+                    dtype=torch.uint8, device=DEV)
+    g = sdm.linear_bwd(x, w, dy, z=z, act=1, want_dx=False, want_dw=False, want_dbias=True, workspace=ws)
+    planes = (1 if bf16 else 3) * 640 * 128 * 2
+    assert (ws[:planes] == 0xA5).all() and not (ws == 0xA5).all()
+    assert torch.equal(g["dbias"], sdm.linear_bwd(x, w, dy, z=z, act=1, want_dbias=True)["dbias"])
