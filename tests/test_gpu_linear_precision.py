@@ -11,7 +11,7 @@ import torch
 
 from paper_2607_07386_amd import sdm
 from tests.gpu_util import DEV
-from tests.test_gpu_linear import ACTS, case, close, flat, reference
+from tests.test_gpu_linear import ACTS, SHAPES, case, close, flat, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -113,3 +113,20 @@ def test_bias_gradient_alone_writes_no_dz(bf16):
     planes = (1 if bf16 else 3) * 640 * 128 * 2
     assert (ws[:planes] == 0xA5).all() and not (ws == 0xA5).all()
     assert torch.equal(g["dbias"], sdm.linear_bwd(x, w, dy, z=z, act=1, want_dbias=True)["dbias"])
+
+
+@pytest.mark.parametrize("shape", SHAPES + [(1, 5000, 136, 16, 0, 0), (1, 3000, 72, 64, 0, 0), (1, 2000, 68, 33, 17, 3)])
+def test_fp32_products_lose_no_part(shape):
+    """All fp32, at a tolerance that the loss of any one product of parts exceeds up to 5,000 terms (tests/test_linear_host_parts.py)."""
+    B, T, K, N, hin, hout = shape
+    x, w, bias, _, dy = case(B, T, K, N, hin, hout, False)
+    for act in (0, 1, 2):
+        y, z = sdm.linear(x, w, bias, act=act, heads=hout, want_z=True)
+        ry, rz = reference(x.double(), w.double(), bias.double(), act, None, hout)
+        close(z, rz, "z", f32_tol(K))
+        close(y, ry, "y", f32_tol(K) if act == 0 else 2 * f32_tol(K))     # a slope of at most 1.1, and its own roundings
+    g = sdm.linear_bwd(x, w, dy, want_dbias=True)
+    dx, dw, dbias, _ = definition_gradients(x, w, bias, dy, 0, hin, hout)
+    close(g["dx"], dx, "dx", f32_tol(N))
+    close(g["dw"], dw, "dw", f32_tol(B * T))
+    close(g["dbias"], dbias, "dbias", f32_tol(B * T))
