@@ -677,16 +677,21 @@ hipError_t launch_scan_tiles(const GdnArgs& a, hipStream_t st) {
 
 // Column tiles to a workgroup: as many as leave a workgroup to every compute unit. More
 // share one staging of the chunk, but also one LDS, whose reads then set the pace.
+constexpr int scan_most(int ktn, bool f32) { return ktn == 2 ? 4 : ktn == 4 ? (f32 ? 2 : 4) : f32 ? 1 : 2; }   // what LDS holds
+int scan_nct(int64_t tiles, int most) {
+    const int64_t cus = sdm_device_simds() / 4;
+    return most >= 4 && tiles >= 4 * cus ? 4 : most >= 2 && tiles >= 2 * cus ? 2 : 1;
+}
 template <typename VT, int KTN, int MODE>
 hipError_t launch_scan_halves(const GdnArgs& a, hipStream_t st) {
-    constexpr int MOST = KTN == 2 ? 4 : KTN == 4 && sizeof(VT) == 2 ? 4 : KTN == 8 && sizeof(VT) == 4 ? 1 : 2;   // what LDS holds
+    constexpr int MOST = scan_most(KTN, sizeof(VT) == 4);
     const int64_t cols = (a.dv + 15) / 16 + (MODE == 2 ? (a.dk + 15) / 16 : 0);
-    const int64_t tiles = cols * a.B * a.H * (MODE == 2 ? a.segs - 1 : a.segs), cus = sdm_device_simds() / 4;
+    const int nct = scan_nct(cols * a.B * a.H * (MODE == 2 ? a.segs - 1 : a.segs), MOST);
     if constexpr (MOST == 4) {
-        if (tiles >= 4 * cus) return launch_scan_tiles<VT, KTN, 4, MODE>(a, st);
+        if (nct == 4) return launch_scan_tiles<VT, KTN, 4, MODE>(a, st);
     }
     if constexpr (MOST >= 2) {
-        if (tiles >= 2 * cus) return launch_scan_tiles<VT, KTN, 2, MODE>(a, st);
+        if (nct == 2) return launch_scan_tiles<VT, KTN, 2, MODE>(a, st);
     }
     return launch_scan_tiles<VT, KTN, 1, MODE>(a, st);
 }
@@ -700,6 +705,37 @@ hipError_t launch_scan(const GdnArgs& a, hipStream_t st) {
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     return launch_scan_halves<VT, KTN, SAVE ? 1 : 0>(a, st);
+}
+
+// Time of a chunk of `streams` streams of `cols` column tiles each, in chunks of one workgroup of one tile:
+// the rounds of workgroups, a compute unit holding one, by what a chunk of two and of four tiles takes.
+double scan_chunk_time(int64_t cols, int64_t streams, int most) {
+    const int64_t cus = sdm_device_simds() / 4;
+    const int nct = scan_nct(cols * streams, most);
+    const int64_t wgs = (cols + nct - 1) / nct * streams;
+    return (double)((wgs + cus - 1) / cus) * (nct == 4 ? 1.3 : nct == 2 ? 1.1 : 1.0);
+}
+
+// Segments of a sequence of nC chunks.  Few streams leave the device idle while chunk follows chunk.  Segments
+// side by side first need each one's end, from the zero state and from the unit vectors (d_k / 16 more tiles;
+// such a chunk takes 0.65 of the time, 0.35 where Q would come straight from memory), and the joins, two
+// chunks' time each; then they run as many times fewer chunks in a row.  Five of 16 chunks or more,
+// where that sum is below 0.92 of one pass.  Measured with and without at 390 shapes (either type, d_k
+// 64 to 256, d_v 16 to 1024, 1 to 204 streams, 5,120 to 65,536 tokens): the sum is off by 12% in the mean, no
+// shape that it takes was slower, and of those it leaves one would gain 16%, three 4%.  16 streams of 65,536 tokens, bf16,
+// 128 x 128: 3.8 ms in one, 1.65 in eight; fp32, 256 x 128, 16,384 tokens: 5.1 ms either way, left in one; of
+// 24 streams 5.2 and 7.4.
+int gdn_segments(int64_t BH, int64_t nC, int dk, int dv, bool f32) {
+    const int ktn = dk <= 64 ? 2 : dk <= 128 ? 4 : 8, most = scan_most(ktn, f32);
+    const bool direct = f32 ? ktn >= 4 : ktn == 8;
+    const int64_t cols = (dv + 15) / 16, tiles = cols * BH, room = tiles > 0 ? 4 * (sdm_device_simds() / 4) / tiles : 0;
+    int64_t n = std::min<int64_t>(std::min<int64_t>(room, nC / 16), 64);
+    if (n < 5) return 1;
+    const int64_t len = (nC + n - 1) / n;
+    n = (nC + len - 1) / len;
+    const double in_parts = len * ((direct ? 0.35 : 0.65) * scan_chunk_time(cols + (dk + 15) / 16, BH * (n - 1), most) +
+                                   scan_chunk_time(cols, BH * n, most)) + 2.0 * (n - 1);
+    return in_parts < 0.92 * nC * scan_chunk_time(cols, BH, most) ? (int)n : 1;
 }
 
 }  // namespace
@@ -719,14 +755,7 @@ GdnWs gdn_ws(int B, int Hk, int H, int T, int dk, int dv, int in_dtype, bool bac
     w.vec = take(n * GDN_VEC * 64 * 4);
     w.tf = take(n * GDN_BLKS * 3 * GDN_FRAG * 2);
     w.pf = take(n * GDN_BLKS * 3 * GDN_FRAG * 2);
-    // Few streams leave the device idle while chunk follows chunk.  Segments of the sequence side by
-    // side cost 2.2 times the work (each one's end is found from the zero state and from the unit
-    // vectors first) and then run as many times fewer chunks in a row: worth it from five
-    // segments on, of 16 chunks or more (16 streams of 65,536 tokens: 3.7 ms in one, 1.5 in eight).
-    w.segs = 1;
-    const int64_t tiles = (int64_t)((dv + 15) / 16) * B * H, room = tiles > 0 ? 4 * (sdm_device_simds() / 4) / tiles : 0;
-    const int64_t segs = std::min<int64_t>(std::min<int64_t>(room, nC / 16), 64);
-    if (!backward && segs >= 5) w.segs = (int)segs;
+    w.segs = backward ? 1 : gdn_segments((int64_t)B * H, (int64_t)nC, dk, dv, f32);
     w.seg_len = (int)((nC + w.segs - 1) / w.segs);
     if (w.seg_len > 0) w.segs = (int)((nC + w.seg_len - 1) / w.seg_len);
     if (w.segs > 1) {
