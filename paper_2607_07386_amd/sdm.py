@@ -749,7 +749,7 @@ class Preactivation(torch.Tensor):
 
     def to(self, *args, **kwargs):
         t = super().to(*args, **kwargs)
-        return t if self.rest is None or t.element_size() <= 2 else t + self.rest.to(t.device, t.dtype)
+        return t + self.rest.to(t.device, t.dtype) if self.rest is not None and t.dtype in (torch.float32, torch.float64) else t
 
     def float(self):
         return self.to(torch.float32)

@@ -21,6 +21,7 @@ def test_widened_it_is_the_value_that_was_kept():
     # narrow, it is the rounded value, and what torch makes of it is a plain tensor
     for got in (z + 0, z.clone(), z[:1], z.detach(), torch.cat([z, z]), z.to(torch.bfloat16, copy=True)):
         assert type(got) is torch.Tensor and got.dtype == torch.bfloat16
+    assert torch.equal(z.to(torch.int32), rounded.to(torch.int32)) and torch.equal(z.to(torch.bool), rounded.to(torch.bool))
     assert torch.equal(z.clone(), rounded) and z.dtype == torch.bfloat16 and z.shape == (2, 5, 12)
 
 
