@@ -12,7 +12,7 @@
 // accumulators, which is faster than the fp32 matrix instruction.  Measured: 8192^3 in
 // bf16 0.85 ms, 1.29 PFLOP/s (the library's product 1.66); fp32 4096^3 200 TFLOP/s (the
 // library's 151); a layer's projection, 16,384 tokens of 2048 to 2048, 126 us (the library 95),
-// with SiLU, head-major, 152 us, 0.90 PFLOP/s.
+// with SiLU, head-major, 154 us, 0.89 PFLOP/s.
 // There the 32 steps of a tile are few beside its start and its epilogue, and 512
 // tiles make two rounds of 256 compute units in which neither overlaps the next.
 #include <algorithm>
@@ -600,7 +600,7 @@ __device__ __forceinline__ void put_parts(bf16_t* p, int64_t plane, const float 
 }
 
 // An fp32 matrix as bf16 planes [rows][ld], zeros past its end (both multiples of 64).  16,384 x 2048
-// head-major, rounded: 32 us, 201 MB (part of it from the caches).
+// head-major in two parts: 42 us, 268 MB (part of it from the caches).
 template <int NP>
 __global__ __launch_bounds__(256) void linear_parts_kernel(LinMat m, int rows, int ld, bf16_t* out, int64_t plane) {
     const int c = (blockIdx.x * 32 + (threadIdx.x & 31)) * 8;
