@@ -757,6 +757,11 @@ class Preactivation(torch.Tensor):
     def double(self):
         return self.to(torch.float64)
 
+    def __deepcopy__(self, memo):
+        z = memo[id(self)] = self.clone().as_subclass(Preactivation)
+        z.rest = None if self.rest is None else self.rest.clone()
+        return z
+
 
 def linear_workspace(x, w) -> torch.Tensor:
     B, T, K, N, _ = _check_linear(x, w)

@@ -1,4 +1,7 @@
 """What a kept pre-activation carries, and which gradients are refused without it (CPU only: nothing reaches a kernel)."""
+import copy
+import io
+
 import pytest
 import torch
 
@@ -23,6 +26,29 @@ def test_widened_it_is_the_value_that_was_kept():
         assert type(got) is torch.Tensor and got.dtype == torch.bfloat16
     assert torch.equal(z.to(torch.int32), rounded.to(torch.int32)) and torch.equal(z.to(torch.bool), rounded.to(torch.bool))
     assert torch.equal(z.clone(), rounded) and z.dtype == torch.bfloat16 and z.shape == (2, 5, 12)
+
+
+def test_copied_or_saved_whole_it_keeps_the_rest():
+    _, z = kept()
+    f = io.BytesIO()
+    torch.save(z, f)
+    f.seek(0)
+    loaded = torch.load(f, weights_only=False)      # this test's own bytes
+    for got in (copy.copy(z), copy.deepcopy(z), loaded):
+        assert type(got) is sdm.Preactivation and torch.equal(got.rest, z.rest) and torch.equal(got.clone(), z.clone())
+
+    class Saves(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            ctx.save_for_backward(z)
+            return x * 2
+
+        @staticmethod
+        def backward(ctx, g):
+            assert type(ctx.saved_tensors[0]) is sdm.Preactivation and torch.equal(ctx.saved_tensors[0].rest, z.rest)
+            return g * 2
+
+    Saves.apply(torch.ones(3, requires_grad=True)).sum().backward()
 
 
 def args(**kw):
