@@ -486,9 +486,9 @@ size_t sdm_gdn_bwd_workspace_bytes(int B, int Hk, int H, int T, int d_k, int d_v
  *   dx = dz W,  dw = dz^T x,  dbias[n] = sum over tokens of dz;  the gradient of
  *   residual is dy itself.
  *   dy        laid out as y, in dy_dtype: w's type, or fp32 (as the recurrences'
- *             backwards write their gradients).  dbias sums dz in fp32.  With fp32 x or w
- *             dz enters the products in full; else, with an fp32 dy, to 2^-15 (dx and dw are
- *             bf16); with a bf16 dy it is rounded to bf16.  An fp32 x beside a bf16 w enters
+ *             backwards write their gradients).  dbias sums dz in fp32.  An fp32 dx or dw
+ *             takes dz in full, a bf16 one to 2^-14 where x or dy is fp32; from a bf16 dy
+ *             beside bf16 x and w, dz is rounded to bf16.  An fp32 x beside a bf16 w enters
  *             dw to 2^-15.
  *   z, z_rest as sdm_linear wrote them (z_dtype); NULL with act 0.  With z_rest the
  *             activation's slope is taken at z to 2^-16; without it at the rounded z, whose

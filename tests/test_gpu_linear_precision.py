@@ -56,9 +56,9 @@ def test_bias_gradient_of_the_plain_call(shape, kind, act):
         assert torch.equal(g[name], g2[name]), name
 
 
-MIXED = [  # B, T, K, N, heads in, heads out: few rows, few outputs, tiles, odd sizes, a split depth
+MIXED = [  # B, T, K, N, heads in, heads out: few rows, few outputs, tiles, odd sizes, a split depth, large tiles
     (3, 1, 64, 40, 4, 0), (16, 1, 256, 512, 0, 4), (2, 200, 136, 24, 0, 0), (2, 257, 96, 96, 2, 3), (1, 300, 704, 260, 0, 0),
-    (3, 50, 520, 90, 13, 0), (1, 640, 512, 512, 8, 8), (1, 129, 4096, 130, 0, 0),
+    (3, 50, 520, 90, 13, 0), (1, 640, 512, 512, 8, 8), (1, 129, 4096, 130, 0, 0), (1, 4099, 1032, 2000, 0, 0),
 ]
 
 
